@@ -294,6 +294,86 @@ uint64_t adacc_mask_packed_bytes(uint64_t n);
 int adacc_mask_pack(const void *mask, uint64_t n, void *bits, void *hip_stream);
 int adacc_mask_unpack(const void *bits, uint64_t n, void *mask, void *hip_stream);
 
+/* ---- matrices in microscaled 4-bit floating point, and their products ----
+ * The codes of the calls above are integers, which a product can not read: the tensor is restored first.  The matrix cores
+ * read this format as it is, so that a saved activation of 4.25 bits a value is also what its gradient is computed from.
+ *
+ * Format (MXFP4 of the OCP Microscaling specification 1.0): a row is cut into blocks of 32 consecutive values from its start, the last
+ * one may be short.  A block has one scale 2^e, -127 <= e <= 127, kept as the byte e + 127, and a 4-bit code per value: the sign in
+ * bit 3, and 0, 0.5, 1, 1.5, 2, 3, 4, 6 for 0 ... 7 in bits 0-2.  Restored value = code * 2^e.
+ *   ADACC_MX4_SCALE_FLOOR      2^e = a quarter of the largest power of two <= max|x|; beyond 6 * 2^e a value is held at that
+ *                              (the specification's rule)
+ *   ADACC_MX4_SCALE_FULLRANGE  the smallest 2^e with max|x| <= 6 * 2^e: nothing is held
+ * (e = -127 at least; a block of zeros has byte 0).  A value goes to the nearest code, in the middle between two to the one whose
+ * bit 0 is zero.  A block that holds an Inf or NaN has byte 255 and codes 0: all its values restore to NaN, and
+ * every result that it has a part in is NaN.
+ *
+ * Blob of a matrix [rows, cols] (adacc_mx4_layout; sections on 256-byte boundaries):
+ *   codes   [rows][row_bytes], row_bytes = 64 * ceil(cols / 128); element 2j in the low nibble of byte j, zeros behind the row's end
+ *   scales  [4 * ceil(cols / 128)][scale_pitch], one byte for a block: that of block column c of row i at c * scale_pitch + i;
+ *           scale_pitch = 16 * ceil(rows / 16), the bytes behind the last row are unspecified
+ * A stack of matrices [mats, rows, cols] is the matrix [mats * rows, cols].
+ *
+ * Groups (experts): rows sorted by group; group g has the rows [offsets[g], offsets[g + 1]), any number of them, none included.
+ * offsets is DEVICE memory, groups + 1 int32, ascending; offsets[0] counts as 0, rows from offsets[groups] on belong to no group.  The
+ * host never reads it.  Offsets that do not ascend or lead beyond the rows give unspecified results, and no access outside of the
+ * buffers.  groups = 0, offsets = NULL: no groups.
+ *
+ * Limits (ELIMIT): rows and columns of a blob 2^30, the contraction of a product 2^24, groups 4096.
+ * Sizes of zero: ADACC_OK; nothing is touched if there is no result, a contraction of length zero gives zeros. */
+#define ADACC_MX4_BF16 0 /* types of matrices that are not compressed */
+#define ADACC_MX4_F16 1
+#define ADACC_MX4_F32 2
+#define ADACC_MX4_SCALE_FLOOR 0
+#define ADACC_MX4_SCALE_FULLRANGE 1
+
+typedef struct adacc_mx4_layout {
+  uint64_t codes_off, scales_off, total_bytes;
+  uint64_t row_bytes, scale_pitch;
+} adacc_mx4_layout;
+
+/* Host only, pure.  Errors: ENULL, ELIMIT. */
+int adacc_mx4_layout_of(uint64_t rows, uint64_t cols, adacc_mx4_layout *out);
+
+/* Columns of a blob that holds `rows` rows in groups across: the rows of every group start at a multiple of 128 (so that no block and no
+ * step of a product has rows of two), group after group.  Host only, pure; 0 beyond the limits. */
+uint64_t adacc_mx4_grouped_cols(uint64_t rows, uint32_t groups);
+
+/* src: mats matrices [rows, cols] of `type`, element (i, r, c) at i * mat_stride + r * row_stride + c, at any element's address
+ *   along   (may be NULL) blob [mats * rows, cols]: blocks along the rows
+ *   across  (may be NULL) blob [mats * cols, rows] of the transposed matrices: blocks along the columns of src.  With groups (mats = 1):
+ *           blob [cols, adacc_mx4_grouped_cols(rows, groups)], blocks cut at the groups' first rows; what lies behind the last group's
+ *           positions is not written
+ * Both are made from one reading of src.  Errors: EINVAL, ENULL, ESIZE, EALIGN, ELIMIT, EHIP. */
+int adacc_mx4_compress(uint32_t type, uint32_t scale_rule, const void *src, uint64_t mats, uint64_t rows, uint64_t cols, uint64_t row_stride,
+                       uint64_t mat_stride, const int32_t *offsets, uint32_t groups, void *along, uint64_t along_bytes, void *across,
+                       uint64_t across_bytes, void *hip_stream);
+
+/* dst[r * row_stride + c] of `type` = code * 2^e, rounded to nearest even where the type does not hold it (exact in binary32, and in
+ * bf16 but for values beyond its range). */
+int adacc_mx4_decompress(const void *blob, uint64_t blob_bytes, uint64_t rows, uint64_t cols, void *dst, uint32_t type, uint64_t row_stride,
+                         void *hip_stream);
+
+/* out[i][j] = sum over c of A[i][c] * B[j][c]: A [m, k] and B [n, k] are blobs, the sum is kept in binary32 and rounded once to out_type.
+ * With groups B is [groups * n, k] and row i is multiplied with the n rows of its group; rows of no group give zeros.
+ * The order of a sum depends on m, n, k and groups alone. */
+int adacc_mx4_product(const void *a, uint64_t a_bytes, uint64_t m, const void *b, uint64_t b_bytes, uint64_t n, uint64_t k,
+                      const int32_t *offsets, uint32_t groups, void *out, uint32_t out_type, uint64_t out_stride, void *hip_stream);
+
+/* The same with A = the compressed rows of x (of `type`, row i at i * x_stride).  Few rows are compressed on the way; otherwise into
+ * the workspace: adacc_mx4_linear_workspace_bytes of 256-byte aligned device memory (0: none is needed), no initialisation, may be shared by calls
+ * that follow each other on one stream. */
+uint64_t adacc_mx4_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint32_t groups);
+int adacc_mx4_linear(uint32_t type, uint32_t scale_rule, const void *x, uint64_t m, uint64_t x_stride, const void *b, uint64_t b_bytes,
+                     uint64_t n, uint64_t k, const int32_t *offsets, uint32_t groups, void *out, uint32_t out_type, uint64_t out_stride,
+                     void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* The gradient of the groups' matrices: out[g][i][j] = sum over the rows t of group g of A[i][t] * B[j][t], where A [m, rows] and B [n, rows]
+ * are what adacc_mx4_compress made across the rows with the same offsets.  out: [max(groups, 1)][m][out_stride]; a group without rows gives zeros.
+ * Without groups this is adacc_mx4_product with a contraction over the rows. */
+int adacc_mx4_gradient(const void *a, uint64_t a_bytes, uint64_t m, const void *b, uint64_t b_bytes, uint64_t n, uint64_t rows,
+                       const int32_t *offsets, uint32_t groups, void *out, uint32_t out_type, uint64_t out_stride, void *hip_stream);
+
 /* ---- what the policy maker consumes (Section 3.3: CRate_i in the memory constraint; Section 3.4:
  * the rate is re-evaluated while training, as the number of outliers moves) ----
  * Host only, pure.  Bytes of the blob that carry information for a tensor compressed with `method`

@@ -32,7 +32,9 @@ EXPORTS = ("adacc_layout_of", "adacc_workspace_bytes", "adacc_workspace_init", "
            "adacc_mask_packed_bytes", "adacc_mask_pack", "adacc_mask_unpack", "adacc_compressed_bytes",
            "adacc_channel_compressed_bytes",
            "adacc_channelwise_layout_of", "adacc_channelwise_workspace_bytes", "adacc_channelwise_compress",
-           "adacc_channelwise_decompress")
+           "adacc_channelwise_decompress",
+           "adacc_mx4_layout_of", "adacc_mx4_grouped_cols", "adacc_mx4_compress", "adacc_mx4_decompress", "adacc_mx4_product",
+           "adacc_mx4_linear_workspace_bytes", "adacc_mx4_linear", "adacc_mx4_gradient")
 
 
 class CMethod(ctypes.Structure):
@@ -67,6 +69,10 @@ class CChannelLayout(ctypes.Structure):
 
 class CChannelwiseLayout(ctypes.Structure):
     _fields_ = [("codes_off", ctypes.c_uint64), ("scales_off", ctypes.c_uint64), ("total_bytes", ctypes.c_uint64)]
+
+
+class CMx4Layout(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_uint64) for k in ("codes_off", "scales_off", "total_bytes", "row_bytes", "scale_pitch")]
 
 
 @dataclass
@@ -228,6 +234,22 @@ def lib():
         L.adacc_channelwise_compress.restype = ci
         L.adacc_channelwise_decompress.argtypes = [u32, u32, vp, u64, u64, u32, vp, ci, vp]
         L.adacc_channelwise_decompress.restype = ci
+        L.adacc_mx4_layout_of.argtypes = [u64, u64, ctypes.POINTER(CMx4Layout)]
+        L.adacc_mx4_layout_of.restype = ci
+        L.adacc_mx4_grouped_cols.argtypes = [u64, u32]
+        L.adacc_mx4_grouped_cols.restype = u64
+        L.adacc_mx4_compress.argtypes = [u32, u32, vp, u64, u64, u64, u64, u64, vp, u32, vp, u64, vp, u64, vp]
+        L.adacc_mx4_compress.restype = ci
+        L.adacc_mx4_decompress.argtypes = [vp, u64, u64, u64, vp, u32, u64, vp]
+        L.adacc_mx4_decompress.restype = ci
+        L.adacc_mx4_product.argtypes = [vp, u64, u64, vp, u64, u64, u64, vp, u32, vp, u32, u64, vp]
+        L.adacc_mx4_product.restype = ci
+        L.adacc_mx4_linear_workspace_bytes.argtypes = [u64, u64, u64, u32]
+        L.adacc_mx4_linear_workspace_bytes.restype = u64
+        L.adacc_mx4_linear.argtypes = [u32, u32, vp, u64, u64, vp, u64, u64, u64, vp, u32, vp, u32, u64, vp, u64, vp]
+        L.adacc_mx4_linear.restype = ci
+        L.adacc_mx4_gradient.argtypes = [vp, u64, u64, vp, u64, u64, u64, vp, u32, vp, u32, u64, vp]
+        L.adacc_mx4_gradient.restype = ci
         L.adacc_version.argtypes = []
         L.adacc_version.restype = ctypes.c_char_p
         _lib = L
@@ -608,6 +630,122 @@ def mask_unpack(bits, mask, n=None, stream=None):
     if _nbytes(bits) < mask_packed_bytes(n) or _nbytes(mask) < n:
         raise AdaccError(ESIZE, "adacc_mask_unpack")
     _check(lib().adacc_mask_unpack(_ptr(bits), n, _ptr(mask), _stream(stream)), "adacc_mask_unpack")
+
+
+# ---------------------------------------------------------------- microscaled 4-bit matrices and their products
+MX4_BF16, MX4_F16, MX4_F32 = 0, 1, 2
+MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE = 0, 1
+
+
+def mx4_layout_of(rows: int, cols: int) -> CMx4Layout:
+    L = CMx4Layout()
+    _check(lib().adacc_mx4_layout_of(rows, cols, ctypes.byref(L)), "adacc_mx4_layout_of")
+    return L
+
+
+def mx4_grouped_cols(rows: int, groups: int) -> int:
+    """Columns of a blob that holds `rows` rows, sorted into groups, across (mx4_compress with offsets)."""
+    return int(lib().adacc_mx4_grouped_cols(rows, groups))
+
+
+def _mx4_type(t):
+    import torch
+    try:
+        return {torch.bfloat16: MX4_BF16, torch.float16: MX4_F16, torch.float32: MX4_F32}[t.dtype]
+    except KeyError:
+        raise TypeError(f"bfloat16, float16 or float32 is needed, not {t.dtype}") from None
+
+
+def _mx4_rows(t, what):
+    """The stride between the rows of a matrix whose rows lie in one piece each."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a matrix with adjacent columns")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _mx4_groups(offsets):
+    """(device pointer, number of groups) of an int32 tensor of groups + 1 offsets, or of None."""
+    import torch
+    if offsets is None:
+        return None, 0
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.numel() < 2:
+        raise TypeError("offsets must be a contiguous int32 tensor of one offset more than there are groups")
+    return offsets.data_ptr(), offsets.numel() - 1
+
+
+def _mx4_blob(blob):
+    return (None, 0) if blob is None else (_ptr(blob), _nbytes(blob))
+
+
+def mx4_compress(src, along=None, across=None, offsets=None, scale_rule=MX4_SCALE_FLOOR, stream=None):
+    """src: a matrix [rows, cols], or a stack [mats, rows, cols] of them, with adjacent columns, of bfloat16, float16 or float32.
+    along: blob of [mats * rows, cols], blocks along the rows; across: blob of [mats * cols, rows] of the transposed matrices, or, with the offsets of
+    groups of rows, of [cols, mx4_grouped_cols(rows, groups)].  Either may be None."""
+    kind = _mx4_type(src)
+    if src.dim() not in (2, 3) or (src.shape[-1] > 1 and src.stride(-1) != 1):
+        raise ValueError("src must be a matrix or a stack of matrices with adjacent columns")
+    mats = src.shape[0] if src.dim() == 3 else 1
+    rows, cols = src.shape[-2:]
+    row_stride = src.stride(-2) if rows > 1 else cols
+    mat_stride = src.stride(0) if src.dim() == 3 and mats > 1 else 0
+    off, groups = _mx4_groups(offsets)
+    _check(lib().adacc_mx4_compress(kind, scale_rule, _ptr(src), mats, rows, cols, row_stride, mat_stride, off, groups, *_mx4_blob(along),
+                                    *_mx4_blob(across), _stream(stream)), "adacc_mx4_compress")
+
+
+def mx4_decompress(blob, dst, stream=None):
+    """dst: a matrix with adjacent columns, of the blob's shape."""
+    kind = _mx4_type(dst)
+    stride = _mx4_rows(dst, "dst")
+    _check(lib().adacc_mx4_decompress(*_mx4_blob(blob), dst.shape[0], dst.shape[1], _ptr(dst), kind, stride, _stream(stream)),
+           "adacc_mx4_decompress")
+
+
+def mx4_product(a, b, k: int, out, offsets=None, stream=None):
+    """out [m, n] = A B^T of the blobs A [m, k] and B [n, k]; with the offsets of groups of rows, B is [groups * n, k]."""
+    kind = _mx4_type(out)
+    stride = _mx4_rows(out, "out")
+    off, groups = _mx4_groups(offsets)
+    m, n = out.shape
+    _check(lib().adacc_mx4_product(*_mx4_blob(a), m, *_mx4_blob(b), n, k, off, groups, _ptr(out), kind, max(stride, n), _stream(stream)),
+           "adacc_mx4_product")
+
+
+def mx4_linear_workspace_bytes(m: int, n: int, k: int, groups: int = 0) -> int:
+    return int(lib().adacc_mx4_linear_workspace_bytes(m, n, k, groups))
+
+
+def mx4_linear(x, b, out, offsets=None, workspace=None, scale_rule=MX4_SCALE_FLOOR, stream=None):
+    """out [m, n] = MX4(x) B^T for the matrix x [m, k] and the blob B [n, k]; with the offsets of groups of rows, B is [groups * n, k].
+    workspace: a buffer of at least mx4_linear_workspace_bytes."""
+    kind, okind = _mx4_type(x), _mx4_type(out)
+    x_stride, o_stride = _mx4_rows(x, "x"), _mx4_rows(out, "out")
+    off, groups = _mx4_groups(offsets)
+    m, k = x.shape
+    n = out.shape[1]
+    if out.shape[0] != m:
+        raise ValueError(f"out has {out.shape[0]} rows, x has {m}")
+    _check(lib().adacc_mx4_linear(kind, scale_rule, _ptr(x), m, max(x_stride, k), *_mx4_blob(b), n, k, off, groups, _ptr(out), okind,
+                                  max(o_stride, n), *_mx4_blob(workspace), _stream(stream)), "adacc_mx4_linear")
+
+
+def mx4_gradient(a, b, rows: int, out, offsets=None, stream=None):
+    """out [groups, m, n], resp. [m, n] without offsets: sums over the rows of each group of A[i, t] * B[j, t]; A and B are blobs that
+    mx4_compress made across the same `rows` rows with the same offsets."""
+    kind = _mx4_type(out)
+    off, groups = _mx4_groups(offsets)
+    if out.dim() != (3 if groups else 2) or not out.is_contiguous() or (groups and out.shape[0] != groups):
+        raise ValueError("out must be a contiguous [groups, m, n], or [m, n] without offsets")
+    m, n = out.shape[-2:]
+    _check(lib().adacc_mx4_gradient(*_mx4_blob(a), m, *_mx4_blob(b), n, rows, off, groups, _ptr(out), kind, n, _stream(stream)),
+           "adacc_mx4_gradient")
+
+
+def alloc_mx4(rows: int, cols: int, device="cuda"):
+    """(blob, layout) for a matrix [rows, cols]."""
+    import torch
+    L = mx4_layout_of(rows, cols)
+    return torch.empty(int(L.total_bytes), dtype=torch.uint8, device=device), L
 
 
 # ---------------------------------------------------------------- buffer helpers (allocation = plumbing)

@@ -27,6 +27,9 @@ PER_FORMAT = (
 ONCE = (
     "adacc.hip",              # host code, C ABI, utility kernels
     "adacc_k_mask.hip",       # dropout mask, byte <-> bit
+    "adacc_mx4.hip",          # microscaled 4-bit matrices: host code
+    "adacc_k_mx4_convert.hip",  # their compression and restoration
+    "adacc_k_mx4_product.hip",  # their products
 )
 # (source, object suffix, extra flags); the long ones first
 SOURCES = ([(os.path.join(CSRC, f), suffix, flags) for f in PER_FORMAT for suffix, flags in (("", ()), ("_f16", ("-DADACC_F16=1",)))] +
@@ -34,7 +37,7 @@ SOURCES = ([(os.path.join(CSRC, f), suffix, flags) for f in PER_FORMAT for suffi
 HEADERS = [os.path.join(CSRC, f) for f in ("adacc_common.hpp", "adacc_dtype.hpp", "adacc_compress.hpp",
                                            "adacc_decompress.hpp", "adacc_kernels.hpp", "adacc_fn.hpp",
                                            "adacc_channel.hpp", "adacc_generic.hpp", "adacc_long.hpp",
-                                           "adacc_tail.hpp", "adacc_short.hpp")]
+                                           "adacc_tail.hpp", "adacc_short.hpp", "adacc_mx4.hpp")]
 HEADERS.append(os.path.join(ROOT, "include", "adacc.h"))
 OBJDIR = os.path.join(HERE, "_build")
 

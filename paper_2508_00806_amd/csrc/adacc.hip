@@ -402,7 +402,9 @@ static int next_epoch(adacc_workspace* ws, hipStream_t s, uint32_t* epoch) {
   return ADACC_OK;
 }
 
-static int launch_check(const char* what) {
+int hip_result(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+int launch_check(const char* what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? ADACC_OK : hip_fail(e, what);
 }

@@ -94,4 +94,9 @@ typedef void (*MaskFn)(const uint8_t*, uint64_t, uint8_t*);
 MaskFn mask_pack_fn();
 MaskFn mask_unpack_fn();
 
+// ADACC_OK, or ADACC_EHIP with the thread's text for it, after a launch of the kernel `what`
+int launch_check(const char* what);
+// ADACC_EHIP with that text, for the failed call `what`
+int hip_result(hipError_t e, const char* what);
+
 }  // namespace adacc

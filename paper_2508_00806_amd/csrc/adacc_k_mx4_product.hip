@@ -1,0 +1,563 @@
+// Products of matrices in microscaled 4-bit floating point: out[m][n] = sum over k of a[m][k] * b[n][k], both operands' blocks along the
+// contraction.  Dense; with the rows of a sorted by group and a matrix b for each group (experts); and the gradient of such matrices, where
+// the groups cut the contraction.
+//
+// The scaled matrix instructions multiply 32 x 64 by 64 x 32 codes (or 16 x 128 by 128 x 16): a lane gives 16 bytes of codes, one block
+// of a row, and that block's scale byte.  The products of two codes are exact, sums are kept in binary32.
+#include "adacc_mx4.hpp"
+
+namespace adacc {
+
+typedef int mx_i8v __attribute__((ext_vector_type(8)));
+typedef float mx_f16v __attribute__((ext_vector_type(16)));
+typedef float mx_f4v __attribute__((ext_vector_type(4)));
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 mx_f16x2 __attribute__((ext_vector_type(2)));
+typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t mx_u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMxFp4 = 4;  // the matrix instructions' code for E2M1
+
+__device__ __forceinline__ mx_i8v mx_operand(uint4 c) {
+  const mx_i8v v = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};  // (4-bit codes fill the first four registers)
+  return v;
+}
+
+// two values in a 16-bit format, round to nearest even
+__device__ __forceinline__ uint32_t mx_narrow2(uint32_t type, float lo, float hi) {
+  const mx_f32x2 v = {lo, hi};
+  return type == kMxBf16 ? __builtin_bit_cast(uint32_t, __builtin_convertvector(v, mx_bf16x2))
+                         : __builtin_bit_cast(uint32_t, __builtin_convertvector(v, mx_f16x2));
+}
+__device__ __forceinline__ void mx_store1(void* out, uint32_t type, uint64_t at, float v) {
+  if (type == kMxF32) static_cast<float*>(out)[at] = v;
+  else static_cast<uint16_t*>(out)[at] = (uint16_t)mx_narrow2(type, v, v);
+}
+// N (1, 2 or 4) adjacent values, aligned to their size
+template <uint32_t N>
+__device__ __forceinline__ void mx_store(void* out, uint32_t type, uint64_t at, const float (&v)[N]) {
+  if constexpr (N == 1) {
+    mx_store1(out, type, at, v[0]);
+  } else if (type == kMxF32) {
+    float* p = static_cast<float*>(out) + at;
+    if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+  } else {
+    uint16_t* p = static_cast<uint16_t*>(out) + at;
+    if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = make_uint2(mx_narrow2(type, v[0], v[1]), mx_narrow2(type, v[2], v[3]));
+    else *reinterpret_cast<uint32_t*>(p) = mx_narrow2(type, v[0], v[1]);
+  }
+}
+
+// ------------------------------------------------------------------ tiles
+// A workgroup of four wavefronts, two by two, takes a tile of BM x BN results, a wavefront SM x SN tiles of 32 x 32 of it.  Codes and scales
+// of a step (128 columns) go to LDS by loads that pass the registers by, DEPTH steps in a ring.
+//
+// Row SM * r + i of a wavefront's rows is row r of its tile i: the SM scale bytes that a lane needs lie side by side, and so do, on the
+// right-hand side, the SN columns of the results that it holds.
+//
+// LDS holds a row's 64 bytes of a step in four pieces of 16, in slots ordered as they are read (tile i of 32 rows after tile i - 1); the
+// piece c of a slot lies at place c ^ (slot / 4 % 4), so that sixteen lanes that read one piece of adjacent slots meet all banks.
+template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
+struct MxTile {
+  static constexpr uint32_t SM = BM / 64u, SN = BN / 64u;
+  static constexpr uint32_t kA = BM * kMxStepBytes, kB = BN * kMxStepBytes;
+  static constexpr uint32_t kScaleA = kA + kB, kScaleB = kScaleA + 4u * BM;
+  static constexpr uint32_t kStage = kScaleB + 4u * BN;
+  static constexpr uint32_t kLds = kStage * DEPTH;
+  static constexpr uint32_t kCodeLoads = (BM + BN) / 16u / kWavesPerWg;  // of 1 KiB, by each wavefront
+  static constexpr uint32_t kScaleWords = (BM + BN) / 64u;               // loads of 256 bytes by all of them
+  static constexpr uint32_t kScaleLoads = kScaleWords < kWavesPerWg ? 1u : kScaleWords / kWavesPerWg;
+  static constexpr uint32_t kLoads = kCodeLoads + kScaleLoads;
+};
+
+// 16 (or 4) bytes a lane from base + voff to LDS at `lds` and, lane after lane, behind it.  The counter of vector loads counts it; nothing waits for it
+// but mx_wait_loads (the compiler would wait for all such loads before any read of LDS).
+__device__ __forceinline__ void mx_to_lds16(uint32_t lds, const uint8_t* base, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
+}
+__device__ __forceinline__ void mx_to_lds4(uint32_t lds, const uint8_t* base, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
+}
+// a pointer that is the same in all lanes, known to be so
+__device__ __forceinline__ const uint8_t* mx_uniform(const uint8_t* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
+}
+template <uint32_t N>
+__device__ __forceinline__ void mx_wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+// every wavefront's reads of LDS before it have returned, its loads are where mx_wait_loads has left them
+__device__ __forceinline__ void mx_meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+__device__ __forceinline__ uint32_t mx_lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+template <uint32_t S>
+__device__ __forceinline__ uint32_t mx_scales_of(const uint8_t* p) {
+  if constexpr (S == 4) return *reinterpret_cast<const uint32_t*>(p);
+  else if constexpr (S == 2) return *reinterpret_cast<const uint16_t*>(p);
+  else return *p;
+}
+
+template <uint32_t I, uint32_t J>
+__device__ __forceinline__ mx_f16v mx_mfma32(uint4 a, uint4 b, mx_f16v c, uint32_t sa, uint32_t sb) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(a), mx_operand(b), c, kMxFp4, kMxFp4, I, (int)sa, J, (int)sb);
+}
+template <uint32_t SM, uint32_t SN>
+__device__ __forceinline__ void mx_multiply(mx_f16v (&acc)[SM][SN], const uint4 (&a)[SM], const uint4 (&b)[SN], uint32_t sa, uint32_t sb) {
+#define ADACC_MX_AT(I, J) if constexpr (I < SM && J < SN) acc[I % SM][J % SN] = mx_mfma32<I, J>(a[I % SM], b[J % SN], acc[I % SM][J % SN], sa, sb);
+#define ADACC_MX_ROW(I) ADACC_MX_AT(I, 0) ADACC_MX_AT(I, 1) ADACC_MX_AT(I, 2) ADACC_MX_AT(I, 3)
+  ADACC_MX_ROW(0) ADACC_MX_ROW(1) ADACC_MX_ROW(2) ADACC_MX_ROW(3)
+#undef ADACC_MX_ROW
+#undef ADACC_MX_AT
+}
+
+// What a workgroup computes: rows [a_row0, ..) of a by rows [b_row0, ..) of b over steps [step0, step0 + steps)
+struct MxWork {
+  uint32_t a_row0, b_row0;   // multiples of 4
+  uint32_t step0, steps;
+  uint32_t a_first, a_last;  // rows of a that are kept
+  uint32_t b_first, b_last;
+  void* out;                 // the result of (a_first, b_first) ...
+  uint64_t stride;
+};
+
+template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
+__device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w, uint8_t* lds) {
+  using T = MxTile<BM, BN, DEPTH>;
+  constexpr uint32_t SM = T::SM, SN = T::SN;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const uint32_t wm = wave / 2u, wn = wave % 2u;
+  const uint32_t r = lane % 32u, h = lane / 32u;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(mx_lds_address(lds));
+
+  mx_f16v acc[SM][SN];
+#pragma unroll
+  for (uint32_t i = 0; i < SM; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < SN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < 16u; ++e) acc[i][j][e] = 0.0f;
+
+  if (w.steps) {  // (uniform in the workgroup)
+    // what this wavefront loads of every step.  Rows behind the matrix's last read the last one: the results are not kept.
+    const uint8_t* a_base = mx_uniform(p.a.codes + (uint64_t)w.a_row0 * p.a.row_bytes + (uint64_t)w.step0 * kMxStepBytes);
+    const uint8_t* b_base = mx_uniform(p.b.codes + (uint64_t)w.b_row0 * p.b.row_bytes + (uint64_t)w.step0 * kMxStepBytes);
+    const uint8_t* as_base = mx_uniform(p.a.scales + (uint64_t)(4u * w.step0) * p.a.pitch + w.a_row0);
+    const uint8_t* bs_base = mx_uniform(p.b.scales + (uint64_t)(4u * w.step0) * p.b.pitch + w.b_row0);
+    uint32_t code_off[T::kCodeLoads], scale_off[T::kScaleLoads];
+    constexpr uint32_t kALoads = BM / 16u;  // of 1 KiB
+#pragma unroll
+    for (uint32_t i = 0; i < T::kCodeLoads; ++i) {
+      const uint32_t load = i * kWavesPerWg + wave;
+      const bool is_a = load < kALoads;
+      const uint32_t slot = (is_a ? load : load - kALoads) * 16u + lane / 4u;
+      const uint32_t s = is_a ? SM : SN;
+      const uint32_t part = slot / (32u * s), in = slot % (32u * s);
+      const uint32_t row = part * 32u * s + s * (in % 32u) + in / 32u;
+      const uint32_t most = (is_a ? p.a.rows - w.a_row0 : p.b.rows - w.b_row0) - 1u;
+      const uint32_t piece = (lane % 4u) ^ ((slot / 4u) % 4u);
+      code_off[i] = (uint32_t)(min(row, most) * (is_a ? p.a.row_bytes : p.b.row_bytes)) + piece * 16u;
+    }
+    constexpr uint32_t kAWords = BM / 64u;
+#pragma unroll
+    for (uint32_t i = 0; i < T::kScaleLoads; ++i) {
+      const uint32_t load = (i * kWavesPerWg + wave) % T::kScaleWords;
+      const bool is_a = load < kAWords;
+      const uint32_t rows = is_a ? BM : BN;
+      const uint32_t at = (is_a ? load : load - kAWords) * 256u + lane * 4u;
+      const uint64_t pitch = is_a ? p.a.pitch : p.b.pitch;
+      const uint32_t most = (uint32_t)pitch - (is_a ? w.a_row0 : w.b_row0) - 4u;
+      scale_off[i] = (uint32_t)((at / rows) * pitch) + min(at % rows, most);
+    }
+    const auto issue = [&](uint32_t stage, uint32_t step) {
+      const uint32_t to = lds0 + stage * T::kStage;
+#pragma unroll
+      for (uint32_t i = 0; i < T::kCodeLoads; ++i) {
+        const uint32_t load = i * kWavesPerWg + wave;
+        const uint8_t* base = (load < kALoads ? a_base : b_base) + (uint64_t)step * kMxStepBytes;
+        mx_to_lds16(to + load * 1024u, base, code_off[i]);
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < T::kScaleLoads; ++i) {
+        const uint32_t load = (i * kWavesPerWg + wave) % T::kScaleWords;
+        const uint8_t* base = load < kAWords ? as_base + (uint64_t)(4u * step) * p.a.pitch : bs_base + (uint64_t)(4u * step) * p.b.pitch;
+        mx_to_lds4(to + T::kScaleA + load * 256u, base, scale_off[i]);
+      }
+    };
+    // where this lane reads: slot of tile 0, piece 0 and the others
+    uint32_t a_at[2], b_at[2];  // by half of the step
+#pragma unroll
+    for (uint32_t s = 0; s < 2u; ++s) {
+      const uint32_t as = wm * 32u * SM + r, bs = wn * 32u * SN + r;  // (slots of the tiles behind differ by multiples of 32)
+      a_at[s] = as * kMxStepBytes + (((2u * s + h) ^ ((as / 4u) % 4u)) * 16u);
+      b_at[s] = T::kA + bs * kMxStepBytes + (((2u * s + h) ^ ((bs / 4u) % 4u)) * 16u);
+    }
+    const uint32_t as_at = T::kScaleA + h * BM + wm * 32u * SM + SM * r;
+    const uint32_t bs_at = T::kScaleB + h * BN + wn * 32u * SN + SN * r;
+    uint4 a[2][SM], b[2][SN];
+    uint32_t sa[2], sb[2];
+    const auto fetch = [&](uint32_t stage, uint32_t s) {
+      const uint8_t* from = lds + stage * T::kStage;
+#pragma unroll
+      for (uint32_t i = 0; i < SM; ++i) a[s][i] = *reinterpret_cast<const uint4*>(from + a_at[s] + i * 32u * kMxStepBytes);
+#pragma unroll
+      for (uint32_t j = 0; j < SN; ++j) b[s][j] = *reinterpret_cast<const uint4*>(from + b_at[s] + j * 32u * kMxStepBytes);
+      sa[s] = mx_scales_of<SM>(from + as_at + 2u * s * BM);
+      sb[s] = mx_scales_of<SN>(from + bs_at + 2u * s * BN);
+    };
+
+#pragma unroll
+    for (uint32_t d = 0; d < DEPTH; ++d)
+      if (d < w.steps) issue(d, d);
+    if (w.steps >= DEPTH) mx_wait_loads<T::kLoads * (DEPTH - 1u)>();
+    else mx_wait_loads<0>();
+    mx_meet();
+    fetch(0, 0);
+    uint32_t stage = 0;
+    for (uint32_t t = 0; t < w.steps; ++t) {
+      // the first half of step t is in registers
+      fetch(stage, 1);
+      mx_multiply<SM, SN>(acc, a[0], b[0], sa[0], sb[0]);
+      const uint32_t next = stage + 1u == DEPTH ? 0u : stage + 1u;
+      if (t + 1u < w.steps) {
+        // step t + 1 has landed: of the steps behind it at most DEPTH - 2 are on their way
+        if (t + DEPTH <= w.steps) mx_wait_loads<T::kLoads * (DEPTH - 2u)>();
+        else mx_wait_loads<0>();
+        mx_meet();  // ... for every wavefront, and step t has been read by all of them
+        if (t + DEPTH < w.steps) issue(stage, t + DEPTH);
+        fetch(next, 0);
+      }
+      mx_multiply<SM, SN>(acc, a[1], b[1], sa[1], sb[1]);
+      stage = next;
+    }
+  }
+
+  // results: lane (r, h) holds rows 8 * (e / 4) + 4 * h + e % 4 and column r of a tile
+  const uint32_t col0 = w.b_row0 + wn * 32u * SN + SN * r;
+  const bool vec = p.vec && w.b_first % SN == 0u && col0 + SN <= w.b_last && col0 >= w.b_first;
+#pragma unroll
+  for (uint32_t i = 0; i < SM; ++i) {
+#pragma unroll
+    for (uint32_t e = 0; e < 16u; ++e) {
+      const uint32_t row = w.a_row0 + wm * 32u * SM + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
+      if (row < w.a_first || row >= w.a_last) continue;
+      const uint64_t at = (uint64_t)(row - w.a_first) * w.stride;
+      float v[SN];
+#pragma unroll
+      for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
+      if (vec) {
+        mx_store<SN>(w.out, p.out_type, at + (col0 - w.b_first), v);
+      } else {
+#pragma unroll
+        for (uint32_t j = 0; j < SN; ++j)
+          if (col0 + j >= w.b_first && col0 + j < w.b_last) mx_store1(w.out, p.out_type, at + (col0 + j - w.b_first), v[j]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void* mx_out_at(const MxProductArgs& p, uint64_t elems) {
+  return static_cast<uint8_t*>(p.out) + elems * (p.out_type == kMxF32 ? 4u : 2u);
+}
+
+// The eight dies have a second-level cache each and take workgroups in turn: numbered so that a die's are neighbours, tiles go in
+// bands of 8 tile rows, column by column, so that what runs at the same time on a die shares both operands.
+__device__ __forceinline__ uint32_t mx_by_die(uint32_t id, uint32_t total) {
+  constexpr uint32_t kDies = 8u;
+  const uint32_t die = id % kDies, turn = id / kDies, each = total / kDies, more = total % kDies;
+  return die * each + min(die, more) + turn;
+}
+__device__ __forceinline__ void mx_band(uint32_t id, uint32_t m_tiles, uint32_t n_tiles, uint32_t* mt, uint32_t* nt) {
+  constexpr uint32_t kBand = 8u;
+  const uint32_t band = id / (kBand * n_tiles), in = id - band * kBand * n_tiles;
+  const uint32_t high = min(kBand, m_tiles - band * kBand);
+  *nt = in / high;
+  *mt = band * kBand + in - *nt * high;
+}
+
+// ---- rows by groups (or one group): a tile row lies within a group
+template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
+__global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_product_kernel(MxProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
+  uint32_t mt, nt;
+  mx_band(mx_by_die(blockIdx.x, gridDim.x), p.m_tiles, p.n_tiles, &mt, &nt);
+  const MxPlace at = mx_place<true>(p.g, mt, BM);
+  MxWork w;
+  const uint32_t a_low = at.first & ~3u;
+  if (at.last <= at.first || (uint64_t)at.unit * BM >= (uint64_t)(at.last - a_low)) return;
+  w.a_row0 = a_low + at.unit * BM;
+  w.a_first = at.first;
+  w.a_last = at.last;
+  const bool nobody = at.group >= p.g.groups && p.g.offsets != nullptr;  // rows behind the last group: zeros
+  const uint32_t b_first = nobody ? 0u : at.group * p.n;
+  const uint32_t b_low = b_first & ~3u;
+  w.b_row0 = b_low + nt * BN;
+  w.b_first = b_first;
+  w.b_last = b_first + p.n;
+  if (w.b_row0 >= w.b_last) return;
+  w.step0 = 0;
+  w.steps = nobody ? 0u : p.a.steps;
+  w.out = mx_out_at(p, (uint64_t)at.first * p.out_stride);
+  w.stride = p.out_stride;
+  mx_tile<BM, BN, DEPTH>(p, w, mx_lds);
+}
+
+// ---- the contraction by groups: out[g] = sum over the group's padded positions
+template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
+__global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kernel(MxProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
+  const uint32_t per = p.m_tiles * p.n_tiles;
+  const uint32_t id = mx_by_die(blockIdx.x, gridDim.x);
+  const uint32_t group = id / per;
+  uint32_t mt, nt;
+  mx_band(id - group * per, p.m_tiles, p.n_tiles, &mt, &nt);
+  // steps of the groups before this one, and its own
+  const uint32_t lane = threadIdx.x % kWave;
+  uint32_t before = 0;
+  for (uint32_t g0 = 0; g0 < group; g0 += kWave) {
+    const uint32_t i = g0 + lane;
+    uint32_t steps = 0;
+    if (i < group) {
+      const uint32_t first = mx_offset(p.g, i), last = mx_offset(p.g, i + 1u);
+      steps = last > first ? (last - first + kMxStep - 1u) / kMxStep : 0u;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) steps += __shfl_xor(steps, d);
+    before += steps;
+  }
+  const uint32_t first = mx_offset(p.g, group), last = mx_offset(p.g, group + 1u);
+  MxWork w;
+  w.step0 = __builtin_amdgcn_readfirstlane(min(before, p.a.steps));
+  w.steps = __builtin_amdgcn_readfirstlane(last > first ? min((last - first + kMxStep - 1u) / kMxStep, p.a.steps - w.step0) : 0u);
+  w.a_row0 = mt * BM;
+  w.a_first = 0;
+  w.a_last = p.m;
+  w.b_row0 = nt * BN;
+  w.b_first = 0;
+  w.b_last = p.n;
+  w.out = mx_out_at(p, (uint64_t)group * p.out_group);
+  w.stride = p.out_stride;
+  mx_tile<BM, BN, DEPTH>(p, w, mx_lds);
+}
+
+// ------------------------------------------------------------------ few rows
+// What bounds a product of few rows is the reading of b.  A workgroup takes 16 * NS rows of b and up to 16 * MS rows of a; its wavefronts
+// share the contraction, two steps (128 bytes of a row) at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
+// operand registers: lane (r, q) = (lane % 16, lane / 16) reads block q of the step of its row.  Row NS * r + j of b is row r of
+// tile j, as above.
+// SRC: a is compressed on the way (kMxBf16 ... kMxF32): the lane's operand is one block of one row, so it reads 32 values, and no
+// other lane has a part in the block.  kMxReady: a is compressed.
+constexpr uint32_t kMxFewAhead = 2;  // pairs of steps in flight
+
+template <uint32_t S>
+__device__ __forceinline__ uint32_t mx_scales_at(const uint8_t* p) {
+  if constexpr (S == 4) return *reinterpret_cast<const mx_u1u*>(p);
+  else if constexpr (S == 2) return *reinterpret_cast<const mx_h1u*>(p);
+  else return *p;
+}
+template <uint32_t J>
+__device__ __forceinline__ mx_f4v mx_mfma16(uint4 a, uint4 b, mx_f4v c, uint32_t sa, uint32_t sb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(a), mx_operand(b), c, kMxFp4, kMxFp4, 0, (int)sa, J, (int)sb);
+}
+
+__device__ __forceinline__ uint32_t mx_pk_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(mx_u16x2, a), __builtin_bit_cast(mx_u16x2, b)));
+}
+
+// one block of 32 values (`left` of them exist; a multiple of 8 or all) to codes and scale byte
+template <uint32_t TYPE>
+__device__ __forceinline__ uint4 mx_compress_block(const uint8_t* p, int32_t left, uint32_t fullrange, uint32_t* byte) {
+  constexpr uint32_t kLoads = TYPE == kMxF32 ? 8u : 4u;
+  constexpr int32_t kEach = 32 / (int32_t)kLoads;
+  uint4 v[kLoads];
+#pragma unroll
+  for (uint32_t i = 0; i < kLoads; ++i) {
+    v[i] = make_uint4(0u, 0u, 0u, 0u);
+    if ((int32_t)i * kEach < left) {
+      const mx_u4u t = *reinterpret_cast<const mx_u4u*>(p + 16u * i);
+      v[i] = make_uint4(t.x, t.y, t.z, t.w);
+    }
+  }
+  uint32_t most = 0u;
+  if constexpr (TYPE == kMxF32) {
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) most = max(most, max(max(v[i].x & 0x7FFFFFFFu, v[i].y & 0x7FFFFFFFu), max(v[i].z & 0x7FFFFFFFu, v[i].w & 0x7FFFFFFFu)));
+  } else {
+    uint32_t m2 = 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) m2 = mx_pk_max(m2, mx_pk_max(mx_pk_max(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), mx_pk_max(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu)));
+    const uint32_t mag = max(m2 & 0xFFFFu, m2 >> 16);
+    most = TYPE == kMxBf16 ? mag << 16 : __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)mag));
+  }
+  *byte = mx_scale_byte(most, fullrange);
+  const float s = mx_scale_value(*byte);
+  uint32_t o[4];
+#pragma unroll
+  for (uint32_t k = 0; k < 4u; ++k) {
+    uint32_t w = 0u;
+    if constexpr (TYPE == kMxF32) {
+      const uint4 x = v[(2 * k) % kLoads], y = v[(2 * k + 1) % kLoads];
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.x), __uint_as_float(x.y), s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.z), __uint_as_float(x.w), s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(y.x), __uint_as_float(y.y), s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(y.z), __uint_as_float(y.w), s, 3);
+    } else if constexpr (TYPE == kMxBf16) {
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].x), s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].y), s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].z), s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].w), s, 3);
+    } else {
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].x), s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].y), s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].z), s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].w), s, 3);
+    }
+    o[k] = *byte == kMxNanByte ? 0u : w;
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+template <uint32_t MS, uint32_t NS, uint32_t SRC>
+__global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const uint32_t waves = blockDim.x / kWave;
+  const uint32_t nt = blockIdx.x % p.n_tiles, mt = blockIdx.x / p.n_tiles;
+  const MxPlace at = mx_place<false>(p.g, mt, 16u * MS);
+  if ((uint64_t)at.unit * (16u * MS) >= (uint64_t)(at.last - at.first)) return;
+  const uint32_t row0 = at.first + at.unit * (16u * MS);
+  const uint32_t rows = min(at.last - row0, 16u * MS);
+  const bool nobody = at.group >= p.g.groups && p.g.offsets != nullptr;
+  const uint32_t b_first = nobody ? 0u : at.group * p.n;
+  const uint32_t col0 = nt * (16u * NS);  // of the output
+  const uint32_t cols = min(p.n - col0, 16u * NS);
+  const uint32_t r = lane % 16u, q = lane / 16u;
+  const uint32_t steps = nobody ? 0u : p.b.steps;
+
+  mx_f4v acc[MS][NS];
+#pragma unroll
+  for (uint32_t i = 0; i < MS; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < NS; ++j) acc[i][j] = mx_f4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // rows behind the last read the last one (of b: results that are not kept; of a: rows that are not kept)
+  const uint8_t* b_row[NS];
+#pragma unroll
+  for (uint32_t j = 0; j < NS; ++j) b_row[j] = p.b.codes + (uint64_t)(b_first + col0 + min(NS * r + j, cols - 1u)) * p.b.row_bytes + 16u * q;
+  const uint64_t b_scale_row = min((uint64_t)b_first + col0 + NS * r, p.b.pitch - NS);
+  const uint8_t* b_scale = p.b.scales + (uint64_t)q * p.b.pitch + b_scale_row;
+  const uint8_t* a_row[MS];
+  const uint8_t* a_scale[MS];
+  bool a_there[MS];
+#pragma unroll
+  for (uint32_t i = 0; i < MS; ++i) {
+    const uint32_t row = row0 + min(16u * i + r, rows - 1u);
+    a_there[i] = 16u * i + r < rows;
+    if constexpr (SRC == kMxReady) {
+      a_row[i] = p.a.codes + (uint64_t)row * p.a.row_bytes + 16u * q;
+      a_scale[i] = p.a.scales + (uint64_t)q * p.a.pitch + row;
+    } else {
+      constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;
+      a_row[i] = static_cast<const uint8_t*>(p.x) + ((uint64_t)row * p.x_stride + kMxBlock * q) * kBytes;
+      a_scale[i] = nullptr;
+    }
+  }
+  for (uint32_t s0 = 2u * wave; s0 < steps; s0 += 2u * kMxFewAhead * waves) {
+    uint4 b[2 * kMxFewAhead][NS], a[2 * kMxFewAhead][MS];
+    uint32_t sb[2 * kMxFewAhead], sa[2 * kMxFewAhead][MS];
+#pragma unroll
+    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
+      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
+      const uint32_t s = min(want, steps - 1u);
+#pragma unroll
+      for (uint32_t j = 0; j < NS; ++j) {
+        const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b_row[j] + (uint64_t)s * kMxStepBytes));
+        b[u][j] = make_uint4(t.x, t.y, t.z, t.w);
+      }
+      sb[u] = mx_scales_at<NS>(b_scale + (uint64_t)(4u * s) * p.b.pitch);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
+      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
+      const uint32_t s = min(want, steps - 1u);
+#pragma unroll
+      for (uint32_t i = 0; i < MS; ++i) {
+        if constexpr (SRC == kMxReady) {
+          a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + (uint64_t)s * kMxStepBytes);
+          sa[u][i] = a_scale[i][(uint64_t)(4u * s) * p.a.pitch];
+        } else {
+          constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;
+          const int32_t left = (int32_t)p.k - (int32_t)(s * kMxStep + q * kMxBlock);
+          a[u][i] = make_uint4(0u, 0u, 0u, 0u);
+          sa[u][i] = 0u;
+          if (a_there[i]) a[u][i] = mx_compress_block<SRC>(a_row[i] + (uint64_t)s * kMxStep * kBytes, left, p.fullrange, &sa[u][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
+      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
+      if (want < steps) {  // (uniform)
+#pragma unroll
+        for (uint32_t i = 0; i < MS; ++i) {
+#define ADACC_MX_AT(J) if constexpr (J < NS) acc[i][J % NS] = mx_mfma16<J>(a[u][i], b[u][J % NS], acc[i][J % NS], sa[u][i], sb[u]);
+          ADACC_MX_AT(0) ADACC_MX_AT(1) ADACC_MX_AT(2) ADACC_MX_AT(3)
+#undef ADACC_MX_AT
+        }
+      }
+    }
+  }
+  // lane (r, q) holds rows 4 * q + e and column r of a tile; [wave][row][column] in LDS
+  float* sums = reinterpret_cast<float*>(mx_lds);
+  constexpr uint32_t kCols = 16u * NS, kRows = 16u * MS;
+#pragma unroll
+  for (uint32_t i = 0; i < MS; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e)
+#pragma unroll
+      for (uint32_t j = 0; j < NS; ++j) sums[((uint64_t)wave * kRows + 16u * i + 4u * q + e) * kCols + NS * r + j] = acc[i][j][e];
+  __syncthreads();
+  for (uint32_t t = threadIdx.x; t < rows * kCols; t += blockDim.x) {
+    const uint32_t row = t / kCols, col = t % kCols;
+    if (col >= cols) continue;
+    float v = 0.0f;
+    for (uint32_t u = 0; u < waves; ++u) v += sums[(u * kRows + row) * kCols + col];
+    mx_store1(p.out, p.out_type, (uint64_t)(row0 + row) * p.out_stride + col0 + col, v);
+  }
+}
+
+template <uint32_t MS, uint32_t NS>
+static MxProductFn few_of(uint32_t src) {
+  if constexpr (MS == 1) {  // (sixteen rows and fewer are compressed on the way)
+    if (src == kMxBf16) return mx4_few_kernel<MS, NS, kMxBf16>;
+    if (src == kMxF16) return mx4_few_kernel<MS, NS, kMxF16>;
+    if (src == kMxF32) return mx4_few_kernel<MS, NS, kMxF32>;
+  }
+  return mx4_few_kernel<MS, NS, kMxReady>;
+}
+template <uint32_t MS>
+static MxProductFn few_by_columns(uint32_t ns, uint32_t src) {
+  return ns == 1 ? few_of<MS, 1>(src) : ns == 2 ? few_of<MS, 2>(src) : few_of<MS, 4>(src);
+}
+MxProductFn mx4_few_fn(uint32_t ms, uint32_t ns, uint32_t src) {
+  return ms == 1 ? few_by_columns<1>(ns, src) : ms == 2 ? few_by_columns<2>(ns, src) : few_by_columns<4>(ns, src);
+}
+
+constexpr uint32_t kMxDepth = 4;
+MxProductFn mx4_product_fn(uint32_t tile, bool gradient) {
+  if (tile == 256) return gradient ? mx4_gradient_kernel<256, 256, kMxDepth> : mx4_product_kernel<256, 256, kMxDepth>;
+  if (tile == 128) return gradient ? mx4_gradient_kernel<128, 128, kMxDepth> : mx4_product_kernel<128, 128, kMxDepth>;
+  return gradient ? mx4_gradient_kernel<64, 64, kMxDepth> : mx4_product_kernel<64, 64, kMxDepth>;
+}
+uint32_t mx4_product_lds(uint32_t tile) {
+  return tile == 256 ? MxTile<256, 256, kMxDepth>::kLds : tile == 128 ? MxTile<128, 128, kMxDepth>::kLds : MxTile<64, 64, kMxDepth>::kLds;
+}
+
+}  // namespace adacc

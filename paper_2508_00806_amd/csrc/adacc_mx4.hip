@@ -1,0 +1,356 @@
+// libadacc, host code of the microscaled 4-bit matrices and their products (include/adacc.h).  Kernels: adacc_k_mx4_*.hip.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "adacc.h"
+#include "adacc_fn.hpp"
+#include "adacc_mx4.hpp"
+
+namespace adacc {
+
+constexpr uint64_t kMxMaxRows = 1ull << 30;      // of a blob, and columns: kernels count them in 32 bits
+constexpr uint64_t kMxMaxContraction = 1ull << 24;  // 256 rows of codes lie within 2^32 bytes
+constexpr uint64_t kMxMaxGrid = 0x7FFFFFFFull;
+
+static uint64_t mx_align256(uint64_t v) { return (v + 255ull) & ~255ull; }
+static uint64_t mx_over(uint64_t v, uint64_t by) { return (v + by - 1) / by; }
+static bool mx_misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+static uint64_t mx_size(uint32_t type) { return type == ADACC_MX4_F32 ? 4u : 2u; }
+static bool mx_sizes_ok(uint64_t rows, uint64_t cols) { return rows <= kMxMaxRows && cols <= kMxMaxRows; }
+
+static void mx_layout(uint64_t rows, uint64_t cols, adacc_mx4_layout* L) {
+  L->row_bytes = mx_over(cols, kMxStep) * kMxStepBytes;
+  L->scale_pitch = mx_over(rows, 16) * 16;
+  L->codes_off = 0;
+  L->scales_off = mx_align256(rows * L->row_bytes);
+  L->total_bytes = L->scales_off + mx_align256(mx_over(cols, kMxStep) * 4 * L->scale_pitch);
+}
+
+static MxMatrix mx_matrix(const void* blob, uint64_t rows, uint64_t cols) {
+  adacc_mx4_layout L;
+  mx_layout(rows, cols, &L);
+  MxMatrix m;
+  uint8_t* b = static_cast<uint8_t*>(const_cast<void*>(blob));
+  m.codes = b + L.codes_off;
+  m.scales = b + L.scales_off;
+  m.row_bytes = L.row_bytes;
+  m.pitch = L.scale_pitch;
+  m.rows = (uint32_t)rows;
+  m.steps = (uint32_t)mx_over(cols, kMxStep);
+  return m;
+}
+
+// a blob that a call reads or writes
+static int mx_check_blob(const void* blob, uint64_t bytes, uint64_t rows, uint64_t cols) {
+  adacc_mx4_layout L;
+  mx_layout(rows, cols, &L);
+  if (L.total_bytes == 0) return ADACC_OK;
+  if (!blob) return ADACC_ENULL;
+  if (bytes < L.total_bytes) return ADACC_ESIZE;
+  return mx_misaligned(blob, 256) ? ADACC_EALIGN : ADACC_OK;
+}
+
+// rows sorted by group, `per` a tile: no more tiles than this, whatever the offsets are (`lower`: a group's first tile may start up to three rows early).
+// The rows behind the last group count as one more.
+static uint64_t mx_tiles(uint64_t rows, uint32_t groups, uint64_t per, bool lower) {
+  if (groups == 0) return mx_over(rows, per);
+  const uint64_t live = std::min<uint64_t>(groups + 1ull, rows);
+  return (rows + (lower ? 3 * live : 0)) / per + live;
+}
+
+static int mx_check_groups(const int32_t* offsets, uint32_t groups) {
+  if (groups > kMxMaxGroups) return ADACC_ELIMIT;
+  if ((offsets != nullptr) != (groups != 0)) return offsets ? ADACC_EINVAL : ADACC_ENULL;
+  return mx_misaligned(offsets, 4) ? ADACC_EALIGN : ADACC_OK;
+}
+
+static int mx_check_out(const void* out, uint32_t type, uint64_t cols, uint64_t stride) {
+  if (type > ADACC_MX4_F32 || stride < cols) return ADACC_EINVAL;
+  if (!out) return ADACC_ENULL;
+  return mx_misaligned(out, mx_size(type)) ? ADACC_EALIGN : ADACC_OK;
+}
+
+// ------------------------------------------------------------------ which kernel
+struct MxPlan {
+  bool few, ready;    // few rows; the left operand has to be compressed before
+  uint32_t ms, ns, waves;
+  uint32_t tile;
+};
+constexpr uint64_t kMxFewRows = 64;
+
+static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
+  MxPlan p;
+  std::memset(&p, 0, sizeof p);
+  const uint64_t rows = groups ? mx_over(m, groups) : m;  // of a group, on average
+  p.few = rows <= kMxFewRows;
+  if (p.few) {
+    p.ms = rows <= 16 ? 1u : rows <= 32 ? 2u : 4u;
+    const uint64_t m_tiles = groups ? std::min<uint64_t>(groups, m) : mx_over(m, 16 * p.ms);
+    p.ns = mx_over(n, 64) * m_tiles >= 512 ? 4u : mx_over(n, 32) * m_tiles >= 256 ? 2u : 1u;
+    p.waves = (uint32_t)std::min<uint64_t>(kMxFewWaves, std::max<uint64_t>(1, mx_over(k, 4 * kMxStep)));
+    p.ready = p.ms != 1 || k % 8 != 0;
+    return p;
+  }
+  const auto tiles = [&](uint64_t t) { return mx_over(rows, t) * mx_over(n, t) * std::max<uint32_t>(groups, 1u); };
+  p.tile = tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  p.ready = true;
+  return p;
+}
+
+static int mx_launch(MxProductFn fn, uint64_t grid, uint32_t threads, uint32_t lds, hipStream_t s, const MxProductArgs& a, const char* what) {
+  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  if (grid == 0) return ADACC_OK;
+  if (lds > 65536u) {  // more than a launch may ask for unless the kernel has been told (nothing is enqueued by it)
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return hip_result(e, what);
+  }
+  hipLaunchKernelGGL(fn, dim3((uint32_t)grid), dim3(threads), lds, s, a);
+  return launch_check(what);
+}
+
+// a (or x) times b: the operands have been checked
+static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStream_t s) {
+  if (plan.few) {
+    a.n_tiles = (uint32_t)mx_over(a.n, 16 * plan.ns);
+    const uint64_t m_tiles = mx_tiles(a.m, a.g.groups, 16 * plan.ms, false);
+    a.m_tiles = (uint32_t)m_tiles;
+    const uint32_t lds = plan.waves * 16u * plan.ms * 16u * plan.ns * 4u;
+    return mx_launch(mx4_few_fn(plan.ms, plan.ns, src), m_tiles * a.n_tiles, plan.waves * kWave, lds, s, a, "mx4_few_kernel");
+  }
+  const uint64_t m_tiles = mx_tiles(a.m, a.g.groups, plan.tile, true);
+  a.m_tiles = (uint32_t)m_tiles;
+  a.n_tiles = (uint32_t)mx_over(a.n + (a.g.groups && a.n % 4 ? 3 : 0), plan.tile);
+  return mx_launch(mx4_product_fn(plan.tile, false), m_tiles * a.n_tiles, kThreads, mx4_product_lds(plan.tile), s, a, "mx4_product_kernel");
+}
+
+static bool mx_vec(const void* out, uint32_t type, uint64_t stride) { return stride % 4 == 0 && !mx_misaligned(out, 4 * mx_size(type)); }
+
+static void mx_compress_launch_args(uint32_t type, uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols,
+                                    uint64_t row_stride, uint64_t mat_stride, MxCompressArgs* a) {
+  std::memset(a, 0, sizeof *a);
+  a->src = src;
+  a->row_stride = row_stride;
+  a->mat_stride = mat_stride;
+  a->mats = (uint32_t)mats;
+  a->rows = (uint32_t)rows;
+  a->cols = (uint32_t)cols;
+  a->fullrange = scale_rule;
+  a->g.rows = (uint32_t)rows;
+  a->col_tiles = (uint32_t)mx_over(cols, type == ADACC_MX4_F32 ? 256 : 512);
+}
+
+static int mx_compress_along(uint32_t type, MxCompressArgs a, void* blob, hipStream_t s) {
+  if (a.mats > 1 && a.mat_stride == (uint64_t)a.rows * a.row_stride) {  // one after the other: one matrix
+    a.rows *= a.mats;
+    a.mats = 1;
+  }
+  a.along = mx_matrix(blob, (uint64_t)a.mats * a.rows, a.cols);
+  // rows a wavefront: 32 where that leaves 1024 workgroups
+  a.wave_rows = 8;
+  while (a.wave_rows < 32 && mx_over(a.rows, 2ull * a.wave_rows * kWavesPerWg) * a.mats * a.col_tiles >= 1024) a.wave_rows *= 2;
+  a.row_tiles = (uint32_t)mx_over(a.rows, a.wave_rows * kWavesPerWg);
+  const uint64_t grid = (uint64_t)a.row_tiles * a.mats * a.col_tiles;
+  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  const bool narrow = a.cols * mx_size(type) < 16;
+  hipLaunchKernelGGL(mx4_compress_fn(type, true, false, narrow), dim3((uint32_t)grid), dim3(kThreads), 0, s, a);
+  return launch_check("mx4_along_kernel");
+}
+
+}  // namespace adacc
+
+using namespace adacc;
+
+extern "C" {
+
+int adacc_mx4_layout_of(uint64_t rows, uint64_t cols, adacc_mx4_layout* out) {
+  if (!out) return ADACC_ENULL;
+  if (!mx_sizes_ok(rows, cols)) return ADACC_ELIMIT;
+  mx_layout(rows, cols, out);
+  return ADACC_OK;
+}
+
+uint64_t adacc_mx4_grouped_cols(uint64_t rows, uint32_t groups) {
+  if (rows > kMxMaxRows || groups > kMxMaxGroups) return 0;
+  return (rows + (uint64_t)(kMxTileRows - 1) * std::min<uint64_t>(groups, rows)) / kMxTileRows * kMxTileRows;
+}
+
+int adacc_mx4_compress(uint32_t type, uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols, uint64_t row_stride,
+                       uint64_t mat_stride, const int32_t* offsets, uint32_t groups, void* along, uint64_t along_bytes, void* across,
+                       uint64_t across_bytes, void* hip_stream) {
+  if (type > ADACC_MX4_F32 || scale_rule > ADACC_MX4_SCALE_FULLRANGE) return ADACC_EINVAL;
+  if (row_stride < cols || (groups && mats != 1)) return ADACC_EINVAL;
+  if (!mx_sizes_ok(rows, cols) || mats > kMxMaxRows || mats * std::max(rows, cols) > kMxMaxRows) return ADACC_ELIMIT;
+  int rc = mx_check_groups(offsets, groups);
+  if (rc != ADACC_OK) return rc;
+  const uint64_t positions = groups ? adacc_mx4_grouped_cols(rows, groups) : rows;
+  if (positions > kMxMaxRows) return ADACC_ELIMIT;
+  if (!mats || !rows || !cols) return ADACC_OK;
+  if (!src || (!along && !across)) return ADACC_ENULL;
+  if (mx_misaligned(src, mx_size(type))) return ADACC_EALIGN;
+  if (along && (rc = mx_check_blob(along, along_bytes, mats * rows, cols)) != ADACC_OK) return rc;
+  if (across && (rc = mx_check_blob(across, across_bytes, mats * cols, positions)) != ADACC_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  MxCompressArgs a;
+  mx_compress_launch_args(type, scale_rule, src, mats, rows, cols, row_stride, mat_stride, &a);
+  const bool narrow = cols * mx_size(type) < 16;
+  if (!across) return mx_compress_along(type, a, along, s);
+  MxCompressArgs b = a;
+  const bool both = along && !narrow;  // (narrow rows: a pass for either)
+  if (both) b.along = mx_matrix(along, mats * rows, cols);
+  b.across = mx_matrix(across, mats * cols, positions);
+  b.g.offsets = offsets;
+  b.g.groups = groups;
+  const uint64_t row_tiles = mx_tiles(rows, groups, kMxTileRows, false);
+  const uint64_t grid = row_tiles * mats * b.col_tiles;
+  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  b.row_tiles = (uint32_t)row_tiles;
+  hipLaunchKernelGGL(mx4_compress_fn(type, both, true, narrow), dim3((uint32_t)grid), dim3(kThreads), 0, s, b);
+  rc = launch_check("mx4_across_kernel");
+  if (rc != ADACC_OK || both || !along) return rc;
+  return mx_compress_along(type, a, along, s);
+}
+
+int adacc_mx4_decompress(const void* blob, uint64_t blob_bytes, uint64_t rows, uint64_t cols, void* dst, uint32_t type, uint64_t row_stride,
+                         void* hip_stream) {
+  if (type > ADACC_MX4_F32 || row_stride < cols) return ADACC_EINVAL;
+  if (!mx_sizes_ok(rows, cols)) return ADACC_ELIMIT;
+  if (!rows || !cols) return ADACC_OK;
+  if (!dst) return ADACC_ENULL;
+  if (mx_misaligned(dst, mx_size(type))) return ADACC_EALIGN;
+  const int rc = mx_check_blob(blob, blob_bytes, rows, cols);
+  if (rc != ADACC_OK) return rc;
+  MxDecompressArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.m = mx_matrix(blob, rows, cols);
+  a.cols = (uint32_t)cols;
+  a.dst = dst;
+  a.row_stride = row_stride;
+  a.col_tiles = (uint32_t)mx_over(cols, type == ADACC_MX4_F32 ? 256 : 512);
+  a.wave_rows = 8;
+  while (a.wave_rows < 32 && mx_over(rows, 2ull * a.wave_rows * kWavesPerWg) * a.col_tiles >= 1024) a.wave_rows *= 2;
+  const uint64_t grid = mx_over(rows, a.wave_rows * kWavesPerWg) * a.col_tiles;
+  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  hipLaunchKernelGGL(mx4_decompress_fn(type), dim3((uint32_t)grid), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);
+  return launch_check("mx4_restore_kernel");
+}
+
+// what the three products check alike; the left operand is the caller's matter.  b has the rows of every group.
+static int mx_check_product(const void* b, uint64_t b_bytes, uint64_t m, uint64_t n, uint64_t k, const int32_t* offsets, uint32_t groups,
+                            const void* out, uint32_t out_type, uint64_t out_stride) {
+  if (out_type > ADACC_MX4_F32 || out_stride < n) return ADACC_EINVAL;
+  const uint64_t mats = groups ? groups : 1;
+  if (m > kMxMaxRows || n > kMxMaxRows || mats * n > kMxMaxRows || k > kMxMaxContraction) return ADACC_ELIMIT;
+  int rc = mx_check_groups(offsets, groups);
+  if (rc != ADACC_OK || !m || !n) return rc;
+  rc = mx_check_out(out, out_type, n, out_stride);
+  return rc != ADACC_OK ? rc : mx_check_blob(b, b_bytes, mats * n, k);
+}
+
+static void mx_product_args(const void* b, uint64_t m, uint64_t n, uint64_t k, const int32_t* offsets, uint32_t groups, void* out,
+                            uint32_t out_type, uint64_t out_stride, MxProductArgs* p) {
+  std::memset(p, 0, sizeof *p);
+  p->b = mx_matrix(b, (groups ? groups : 1) * n, k);
+  p->out = out;
+  p->out_stride = out_stride;
+  p->out_type = out_type;
+  p->m = (uint32_t)m;
+  p->n = (uint32_t)n;
+  p->k = (uint32_t)k;
+  p->vec = mx_vec(out, out_type, out_stride);
+  p->g.offsets = offsets;
+  p->g.groups = groups;
+  p->g.rows = (uint32_t)m;
+}
+
+int adacc_mx4_product(const void* a, uint64_t a_bytes, uint64_t m, const void* b, uint64_t b_bytes, uint64_t n, uint64_t k,
+                      const int32_t* offsets, uint32_t groups, void* out, uint32_t out_type, uint64_t out_stride, void* hip_stream) {
+  int rc = mx_check_product(b, b_bytes, m, n, k, offsets, groups, out, out_type, out_stride);
+  if (rc != ADACC_OK || !m || !n) return rc;
+  rc = mx_check_blob(a, a_bytes, m, k);
+  if (rc != ADACC_OK) return rc;
+  MxProductArgs p;
+  mx_product_args(b, m, n, k, offsets, groups, out, out_type, out_stride, &p);
+  p.a = mx_matrix(a, m, k);
+  return mx_product(mx_plan(m, n, k, groups), p, kMxReady, static_cast<hipStream_t>(hip_stream));
+}
+
+uint64_t adacc_mx4_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
+  if (!m || !n || m > kMxMaxRows || k > kMxMaxContraction || !mx_plan(m, n, k, groups).ready) return 0;
+  adacc_mx4_layout L;
+  mx_layout(m, k, &L);
+  return L.total_bytes;
+}
+
+int adacc_mx4_linear(uint32_t type, uint32_t scale_rule, const void* x, uint64_t m, uint64_t x_stride, const void* b, uint64_t b_bytes,
+                     uint64_t n, uint64_t k, const int32_t* offsets, uint32_t groups, void* out, uint32_t out_type, uint64_t out_stride,
+                     void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  if (type > ADACC_MX4_F32 || scale_rule > ADACC_MX4_SCALE_FULLRANGE || x_stride < k) return ADACC_EINVAL;
+  int rc = mx_check_product(b, b_bytes, m, n, k, offsets, groups, out, out_type, out_stride);
+  if (rc != ADACC_OK || !m || !n) return rc;
+  if (k && !x) return ADACC_ENULL;
+  if (mx_misaligned(x, mx_size(type))) return ADACC_EALIGN;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const MxPlan plan = mx_plan(m, n, k, groups);
+  MxProductArgs p;
+  mx_product_args(b, m, n, k, offsets, groups, out, out_type, out_stride, &p);
+  if (!plan.ready) {
+    p.x = x;
+    p.x_stride = x_stride;
+    p.fullrange = scale_rule;
+    return mx_product(plan, p, type, s);
+  }
+  rc = mx_check_blob(workspace, workspace_bytes, m, k);
+  if (rc != ADACC_OK) return rc;
+  if (k) {
+    MxCompressArgs c;
+    mx_compress_launch_args(type, scale_rule, x, 1, m, k, x_stride, 0, &c);
+    rc = mx_compress_along(type, c, workspace, s);
+    if (rc != ADACC_OK) return rc;
+  }
+  p.a = mx_matrix(workspace, m, k);
+  return mx_product(plan, p, kMxReady, s);
+}
+
+int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* b, uint64_t b_bytes, uint64_t n, uint64_t rows,
+                       const int32_t* offsets, uint32_t groups, void* out, uint32_t out_type, uint64_t out_stride, void* hip_stream) {
+  if (out_type > ADACC_MX4_F32 || out_stride < n) return ADACC_EINVAL;
+  if (m > kMxMaxRows || n > kMxMaxRows || rows > kMxMaxRows) return ADACC_ELIMIT;
+  int rc = mx_check_groups(offsets, groups);
+  if (rc != ADACC_OK) return rc;
+  const uint64_t positions = groups ? adacc_mx4_grouped_cols(rows, groups) : rows;
+  if (positions > kMxMaxContraction) return ADACC_ELIMIT;
+  if (!m || !n) return ADACC_OK;
+  rc = mx_check_out(out, out_type, n, out_stride);
+  if (rc == ADACC_OK) rc = mx_check_blob(a, a_bytes, m, positions);
+  if (rc == ADACC_OK) rc = mx_check_blob(b, b_bytes, n, positions);
+  if (rc != ADACC_OK) return rc;
+  MxProductArgs p;
+  std::memset(&p, 0, sizeof p);
+  p.a = mx_matrix(a, m, positions);
+  p.b = mx_matrix(b, n, positions);
+  p.out = out;
+  p.out_stride = out_stride;
+  p.out_group = m * out_stride;
+  p.out_type = out_type;
+  p.m = (uint32_t)m;
+  p.n = (uint32_t)n;
+  p.k = (uint32_t)positions;
+  p.vec = mx_vec(out, out_type, out_stride);
+  p.g.offsets = offsets;
+  p.g.groups = groups;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (!groups) {
+    p.g.rows = (uint32_t)m;
+    return mx_product(mx_plan(m, n, positions, 0), p, kMxReady, s);
+  }
+  p.g.rows = (uint32_t)rows;
+  const auto tiles = [&](uint64_t t) { return mx_over(m, t) * mx_over(n, t) * groups; };
+  const uint32_t tile = tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  p.m_tiles = (uint32_t)mx_over(m, tile);
+  p.n_tiles = (uint32_t)mx_over(n, tile);
+  return mx_launch(mx4_product_fn(tile, true), tiles(tile), kThreads, mx4_product_lds(tile), s, p, "mx4_gradient_kernel");
+}
+
+}  // extern "C"

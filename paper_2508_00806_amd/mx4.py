@@ -1,0 +1,170 @@
+"""Matrices in microscaled 4-bit floating point, and layers that compute with them.
+
+`compress` keeps a matrix in 4.25 bits a value (blocks of 32 values, one power of two each); `linear` and `experts` multiply rows of 16 or 32 bits
+with weights in that form on the matrix cores.  Given a plain weight, they are differentiable: what is saved for the backward pass is
+not the activation but its 4-bit form, compressed along the tokens while it is read for the product (Section 3.2 compresses saved
+activations and restores them; here the gradient's product reads the codes as they are).
+
+With MX(.) for the blocks along the rows and MXT(.) for those across them, the gradients go straight through the rounding:
+
+    y = MX(x) MX(w)^T        dx = MX(dy) MXT(w)^T        dw = MXT(dy) MXT(x)^T
+
+Plumbing only: buffers and calls; every step runs in the HIP kernels.
+"""
+import torch
+
+from . import (MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE, alloc_mx4, mx4_compress, mx4_decompress, mx4_gradient, mx4_grouped_cols, mx4_linear,
+               mx4_linear_workspace_bytes, mx4_product)
+
+SCALE_RULES = {"floor": MX4_SCALE_FLOOR, "fullrange": MX4_SCALE_FULLRANGE}
+
+
+def _rule(name):
+    try:
+        return SCALE_RULES[name]
+    except KeyError:
+        raise ValueError(f"scale_rule is one of {', '.join(SCALE_RULES)}, not {name!r}") from None
+
+
+class Mx4Matrix:
+    """A compressed matrix [rows, cols], or a stack [mats, rows, cols] of them, blocks along the rows."""
+    __slots__ = ("blob", "shape")
+
+    def __init__(self, blob, shape):
+        self.blob, self.shape = blob, tuple(shape)
+
+    @property
+    def nbytes(self):
+        return self.blob.numel()
+
+    def restore(self, dtype=torch.bfloat16, out=None):
+        """The matrix of the values that the codes stand for."""
+        out = torch.empty(self.shape, dtype=dtype, device=self.blob.device) if out is None else out
+        if tuple(out.shape) != self.shape:
+            raise ValueError(f"out has shape {tuple(out.shape)}, the matrix {self.shape}")
+        mx4_decompress(self.blob, out.flatten(0, -2), stream=_stream_of(self.blob))
+        return out
+
+
+def _stream_of(t):
+    """The current stream of the tensor's device."""
+    return torch.cuda.current_stream(t.device)
+
+
+def _flat(x):
+    """[..., cols] as a matrix with adjacent columns (a copy only where the strides ask for one)."""
+    x = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
+    return x if x.shape[1] <= 1 or (x.stride(1) == 1 and x.stride(0) >= x.shape[1]) else x.contiguous()
+
+
+def _stack(x):
+    if x.dim() == 2:
+        return _flat(x)
+    if x.dim() != 3:
+        raise ValueError(f"a matrix or a stack of matrices is needed, not {x.dim()} dimensions")
+    plain = x.shape[2] <= 1 or (x.stride(2) == 1 and x.stride(1) >= x.shape[2] and x.stride(0) >= 0)
+    return x if plain else x.contiguous()
+
+
+def _blobs(x, along, across, rule, offsets=None):
+    mats = x.shape[0] if x.dim() == 3 else 1
+    rows, cols = x.shape[-2:]
+    a = alloc_mx4(mats * rows, cols, device=x.device)[0] if along else None
+    positions = rows if offsets is None else mx4_grouped_cols(rows, offsets.numel() - 1)
+    t = alloc_mx4(mats * cols, positions, device=x.device)[0] if across else None
+    mx4_compress(x, a, t, offsets=offsets, scale_rule=rule, stream=_stream_of(x))
+    return a, t
+
+
+def compress(x, scale_rule="floor"):
+    """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension."""
+    x = _stack(x.detach())
+    return Mx4Matrix(_blobs(x, True, False, _rule(scale_rule))[0], x.shape)
+
+
+def compress_both(x, scale_rule="floor"):
+    """(x, x transposed), both compressed, from one reading of x: blocks along the last dimension, and along the one before it."""
+    x = _stack(x.detach())
+    along, across = _blobs(x, True, True, _rule(scale_rule))
+    return Mx4Matrix(along, x.shape), Mx4Matrix(across, (*x.shape[:-2], x.shape[-1], x.shape[-2]))
+
+
+def _serve(x, w, offsets, out_dtype):
+    rows = _flat(x)
+    n, k = w.shape[-2:]
+    groups = 0 if offsets is None else offsets.numel() - 1
+    out = torch.empty((rows.shape[0], n), dtype=out_dtype or x.dtype, device=x.device)
+    need = mx4_linear_workspace_bytes(rows.shape[0], n, k, groups)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    mx4_linear(rows, w.blob, out, offsets=offsets, workspace=ws, stream=_stream_of(x))
+    return out.view(*x.shape[:-1], n)
+
+
+class _Layer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets, out_dtype):
+        rows, w_ = _flat(x), _stack(w)
+        need_dx, need_dw = ctx.needs_input_grad[:2]
+        rule = MX4_SCALE_FLOOR
+        xa, xt = _blobs(rows, True, need_dw, rule, offsets)
+        wa, wt = _blobs(w_, True, need_dx, rule)
+        m, n, k = rows.shape[0], w.shape[-2], w.shape[-1]
+        out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
+        mx4_product(xa, wa, k, out, offsets=offsets, stream=_stream_of(x))
+        ctx.save_for_backward(xt, wt, offsets)
+        ctx.x_shape, ctx.x_dtype, ctx.w_shape, ctx.w_dtype = x.shape, x.dtype, w.shape, w.dtype
+        return out.view(*x.shape[:-1], n)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        xt, wt, offsets = ctx.saved_tensors
+        need_dx, need_dw = ctx.needs_input_grad[:2]
+        n, k = ctx.w_shape[-2:]
+        dy = _flat(dy)
+        ga, gt = _blobs(dy, need_dx, need_dw, MX4_SCALE_FLOOR, offsets)
+        dx = dw = None
+        if need_dx:
+            dx = torch.empty((dy.shape[0], k), dtype=ctx.x_dtype, device=dy.device)
+            mx4_product(ga, wt, n, dx, offsets=offsets, stream=_stream_of(dy))
+            dx = dx.view(ctx.x_shape)
+        if need_dw:
+            dw = torch.empty(ctx.w_shape, dtype=ctx.w_dtype, device=dy.device)
+            mx4_gradient(gt, xt, dy.shape[0], dw, offsets=offsets, stream=_stream_of(dy))
+        return dx, dw, None, None
+
+
+def _check_operands(x, w, mats):
+    if len(w.shape) != (3 if mats else 2):
+        raise ValueError(f"the weight must have {3 if mats else 2} dimensions, not {len(w.shape)}")
+    if x.dim() < 1 or x.shape[-1] != w.shape[-1]:
+        raise ValueError(f"rows of {x.shape[-1] if x.dim() else 0} values do not fit a weight of shape {tuple(w.shape)}")
+
+
+def linear(x, weight, out_dtype=None):
+    """x [..., k] times weight [n, k], both in microscaled 4-bit floating point: [..., n] of x's type, or of out_dtype.
+
+    weight: an `Mx4Matrix` (serving: no gradient), or a tensor of bfloat16, float16 or float32, which is compressed by the call; gradients
+    then reach x and weight, each in its own type."""
+    _check_operands(x, weight, False)
+    if isinstance(weight, Mx4Matrix):
+        return _serve(x.detach(), weight, None, out_dtype)
+    return _Layer.apply(x, weight, None, out_dtype)
+
+
+def experts(x, offsets, weight, out_dtype=None):
+    """x [rows, k], rows sorted by expert, times the expert's own weight [n, k]: [rows, n].
+
+    offsets: int32 tensor of experts + 1 entries on x's device; expert e has the rows offsets[e] to offsets[e + 1] (none, if they are equal).  It is
+    read on the device, so nothing waits for it.  Rows behind the last expert's give zeros.  weight: an `Mx4Matrix` of shape
+    [experts, n, k], or a tensor of it; gradients as in `linear`."""
+    _check_operands(x, weight, True)
+    if x.dim() != 2:
+        raise ValueError("x must be a matrix")
+    if offsets.device != x.device:
+        raise ValueError("offsets must be on the device of x")
+    if offsets.numel() != weight.shape[0] + 1:
+        raise ValueError(f"{weight.shape[0]} experts need {weight.shape[0] + 1} offsets, not {offsets.numel()}")
+    if isinstance(weight, Mx4Matrix):
+        return _serve(x.detach(), weight, offsets, out_dtype)
+    return _Layer.apply(x, weight, offsets, out_dtype)
