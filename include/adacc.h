@@ -309,7 +309,8 @@ int adacc_mask_unpack(const void *bits, uint64_t n, void *mask, void *hip_stream
  * every result that it has a part in is NaN.
  *
  * Blob of a matrix [rows, cols] (adacc_mx4_layout; sections on 256-byte boundaries):
- *   codes   [rows][row_bytes], row_bytes = 64 * ceil(cols / 128); element 2j in the low nibble of byte j, zeros behind the row's end
+ *   codes   [ceil(cols / 128)][rows][64]: 128 columns of all rows, then the next; of the 128, element 2j in the low nibble of byte j, 2j + 1
+ *           in the high one; zeros behind the row's end.  step_bytes = 64 * rows
  *   scales  [4 * ceil(cols / 128)][scale_pitch], one byte for a block: that of block column c of row i at c * scale_pitch + i;
  *           scale_pitch = 16 * ceil(rows / 16), the bytes behind the last row are unspecified
  * A stack of matrices [mats, rows, cols] is the matrix [mats * rows, cols].
@@ -319,7 +320,7 @@ int adacc_mask_unpack(const void *bits, uint64_t n, void *mask, void *hip_stream
  * host never reads it.  Offsets that do not ascend or lead beyond the rows give unspecified results, and no access outside of the
  * buffers.  groups = 0, offsets = NULL: no groups.
  *
- * Limits (ELIMIT): rows and columns of a blob 2^30, the contraction of a product 2^24, groups 4096.
+ * Limits (ELIMIT): rows and columns of a blob 2^30, groups 4096.
  * Sizes of zero: ADACC_OK; nothing is touched if there is no result, a contraction of length zero gives zeros. */
 #define ADACC_MX4_BF16 0 /* types of matrices that are not compressed */
 #define ADACC_MX4_F16 1
@@ -329,7 +330,7 @@ int adacc_mask_unpack(const void *bits, uint64_t n, void *mask, void *hip_stream
 
 typedef struct adacc_mx4_layout {
   uint64_t codes_off, scales_off, total_bytes;
-  uint64_t row_bytes, scale_pitch;
+  uint64_t step_bytes, scale_pitch;
 } adacc_mx4_layout;
 
 /* Host only, pure.  Errors: ENULL, ELIMIT. */

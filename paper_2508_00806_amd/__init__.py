@@ -72,7 +72,7 @@ class CChannelwiseLayout(ctypes.Structure):
 
 
 class CMx4Layout(ctypes.Structure):
-    _fields_ = [(k, ctypes.c_uint64) for k in ("codes_off", "scales_off", "total_bytes", "row_bytes", "scale_pitch")]
+    _fields_ = [(k, ctypes.c_uint64) for k in ("codes_off", "scales_off", "total_bytes", "step_bytes", "scale_pitch")]
 
 
 @dataclass

@@ -143,7 +143,7 @@ __device__ __forceinline__ uint64_t mx_rows8(const uint4* raw, const MxMatrix& m
     bytes |= (uint64_t)byte << (8u * i);
     const uint32_t c = mx_row_codes<TYPE>(raw[i], byte);
     if (inside && i < count) {
-      uint8_t* p = m.codes + (row0 + i) * m.row_bytes + col / 2u;
+      uint8_t* p = m.codes + (uint64_t)(col / kMxStep) * m.step_bytes + (row0 + i) * kMxStepBytes + col % kMxStep / 2u;
       if constexpr (E::V == 8u) __builtin_nontemporal_store(c, reinterpret_cast<uint32_t*>(p));
       else __builtin_nontemporal_store((uint16_t)c, reinterpret_cast<uint16_t*>(p));
     }
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_across_kernel(MxCompressArgs 
     const uint64_t column = (uint64_t)ct * E::kStrip + c;
     if (column >= a.cols) break;
     const uint4 v = *reinterpret_cast<const uint4*>(turn + (c / V) * kLaneRoom + (c % V) * kMxStepBytes + (threadIdx.x % 4u) * 16u);
-    store_stream16(a.across.codes + (trow + column) * a.across.row_bytes + (uint64_t)step * kMxStepBytes + (threadIdx.x % 4u) * 16u, v);
+    store_stream16(a.across.codes + (uint64_t)step * a.across.step_bytes + (trow + column) * kMxStepBytes + (threadIdx.x % 4u) * 16u, v);
   }
 }
 
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void mx4_restore_kernel(MxDecompressArgs 
   if (row0 >= a.m.rows || col >= a.cols) return;
   const uint32_t rows = min(a.m.rows - row0, a.wave_rows);
   const uint32_t left = a.cols - col;
-  const uint8_t* codes = a.m.codes + (uint64_t)row0 * a.m.row_bytes + col / 2u;
+  const uint8_t* codes = a.m.codes + (uint64_t)(col / kMxStep) * a.m.step_bytes + (uint64_t)row0 * kMxStepBytes + col % kMxStep / 2u;
   const uint8_t* scales = a.m.scales + (uint64_t)(col / kMxBlock) * a.m.pitch + row0;
   uint8_t* dst = static_cast<uint8_t*>(a.dst) + ((uint64_t)row0 * a.row_stride + col) * E::kBytes;
   for (uint32_t r = 0; r < rows; r += 8u) {
@@ -334,8 +334,8 @@ __global__ __launch_bounds__(kThreads) void mx4_restore_kernel(MxDecompressArgs 
 #pragma unroll
     for (uint32_t i = 0; i < 8u; ++i) {
       const uint32_t at = min(r + i, rows - 1u);
-      if constexpr (V == 8u) c[i] = *reinterpret_cast<const uint32_t*>(codes + (uint64_t)at * a.m.row_bytes);
-      else c[i] = *reinterpret_cast<const uint16_t*>(codes + (uint64_t)at * a.m.row_bytes);
+      if constexpr (V == 8u) c[i] = *reinterpret_cast<const uint32_t*>(codes + (uint64_t)at * kMxStepBytes);
+      else c[i] = *reinterpret_cast<const uint16_t*>(codes + (uint64_t)at * kMxStepBytes);
     }
 #pragma unroll
     for (uint32_t i = 0; i < 8u; ++i) {

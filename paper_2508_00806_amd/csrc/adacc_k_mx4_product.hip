@@ -4,6 +4,9 @@
 //
 // The scaled matrix instructions multiply 32 x 64 by 64 x 32 codes (or 16 x 128 by 128 x 16): a lane gives 16 bytes of codes, one block
 // of a row, and that block's scale byte.  The products of two codes are exact, sums are kept in binary32.
+#include <type_traits>
+#include <utility>
+
 #include "adacc_mx4.hpp"
 
 namespace adacc {
@@ -56,11 +59,13 @@ __device__ __forceinline__ void mx_store(void* out, uint32_t type, uint64_t at, 
 // Row SM * r + i of a wavefront's rows is row r of its tile i: the SM scale bytes that a lane needs lie side by side, and so do, on the
 // right-hand side, the SN columns of the results that it holds.
 //
-// LDS holds a row's 64 bytes of a step in four pieces of 16, in slots ordered as they are read (tile i of 32 rows after tile i - 1); the
-// piece c of a slot lies at place c ^ (slot / 4 % 4), so that sixteen lanes that read one piece of adjacent slots meet all banks.
+// A load of a wavefront brings 16 adjacent rows' 64 bytes of a step, one KiB of memory and of LDS, in four pieces of 16 bytes a row.  Within it LDS holds
+// the rows tile by tile (Q = 16 / SM of each), and piece c of a tile's row r at place c ^ (r / 4 % 4), so that sixteen lanes that read one
+// piece of adjacent rows of a tile meet all banks.
 template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
 struct MxTile {
   static constexpr uint32_t SM = BM / 64u, SN = BN / 64u;
+  static constexpr uint32_t QM = 16u / SM, QN = 16u / SN;
   static constexpr uint32_t kA = BM * kMxStepBytes, kB = BN * kMxStepBytes;
   static constexpr uint32_t kScaleA = kA + kB, kScaleB = kScaleA + 4u * BM;
   static constexpr uint32_t kStage = kScaleB + 4u * BN;
@@ -109,13 +114,27 @@ template <uint32_t I, uint32_t J>
 __device__ __forceinline__ mx_f16v mx_mfma32(uint4 a, uint4 b, mx_f16v c, uint32_t sa, uint32_t sb) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(a), mx_operand(b), c, kMxFp4, kMxFp4, I, (int)sa, J, (int)sb);
 }
-template <uint32_t SM, uint32_t SN>
-__device__ __forceinline__ void mx_multiply(mx_f16v (&acc)[SM][SN], const uint4 (&a)[SM], const uint4 (&b)[SN], uint32_t sa, uint32_t sb) {
-#define ADACC_MX_AT(I, J) if constexpr (I < SM && J < SN) acc[I % SM][J % SN] = mx_mfma32<I, J>(a[I % SM], b[J % SN], acc[I % SM][J % SN], sa, sb);
-#define ADACC_MX_ROW(I) ADACC_MX_AT(I, 0) ADACC_MX_AT(I, 1) ADACC_MX_AT(I, 2) ADACC_MX_AT(I, 3)
-  ADACC_MX_ROW(0) ADACC_MX_ROW(1) ADACC_MX_ROW(2) ADACC_MX_ROW(3)
-#undef ADACC_MX_ROW
-#undef ADACC_MX_AT
+// f(0), f(1), ... f(N - 1), with constants
+template <uint32_t N, typename F, uint32_t... I>
+__device__ __forceinline__ void mx_each(F&& f, std::integer_sequence<uint32_t, I...>) {
+  (f(std::integral_constant<uint32_t, I>{}), ...);
+}
+template <uint32_t N, typename F>
+__device__ __forceinline__ void mx_each(F&& f) {
+  mx_each<N>(f, std::make_integer_sequence<uint32_t, N>{});
+}
+// The SM x SN tiles of a half step, with TASKS tasks spread over them: a wavefront issues in order, and the 32 cycles that a matrix
+// instruction takes are the time for everything else.  (All other instructions ahead of the matrix instructions, as the compiler puts
+// them: 4.1k cycles a step in tiles of 256, of which 1k are matrix instructions.)
+template <uint32_t TASKS, uint32_t SM, uint32_t SN, typename F>
+__device__ __forceinline__ void mx_multiply(mx_f16v (&acc)[SM][SN], const uint4 (&a)[SM], const uint4 (&b)[SN], uint32_t sa, uint32_t sb, F&& task) {
+  mx_each<SM * SN>([&](auto q) {
+    constexpr uint32_t Q = decltype(q)::value, I = Q / SN, J = Q % SN;
+    acc[I][J] = mx_mfma32<I, J>(a[I], b[J], acc[I][J], sa, sb);
+    constexpr uint32_t kFrom = Q * TASKS / (SM * SN), kTo = (Q + 1u) * TASKS / (SM * SN);
+    mx_each<kTo - kFrom>([&](auto k) { task(std::integral_constant<uint32_t, kFrom + decltype(k)::value>{}); });
+    __builtin_amdgcn_sched_barrier(0);
+  });
 }
 
 // What a workgroup computes: rows [a_row0, ..) of a by rows [b_row0, ..) of b over steps [step0, step0 + steps)
@@ -147,25 +166,25 @@ __device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w,
 
   if (w.steps) {  // (uniform in the workgroup)
     // what this wavefront loads of every step.  Rows behind the matrix's last read the last one: the results are not kept.
-    const uint8_t* a_base = mx_uniform(p.a.codes + (uint64_t)w.a_row0 * p.a.row_bytes + (uint64_t)w.step0 * kMxStepBytes);
-    const uint8_t* b_base = mx_uniform(p.b.codes + (uint64_t)w.b_row0 * p.b.row_bytes + (uint64_t)w.step0 * kMxStepBytes);
+    const uint8_t* a_base = mx_uniform(p.a.codes + (uint64_t)w.step0 * p.a.step_bytes + (uint64_t)w.a_row0 * kMxStepBytes);
+    const uint8_t* b_base = mx_uniform(p.b.codes + (uint64_t)w.step0 * p.b.step_bytes + (uint64_t)w.b_row0 * kMxStepBytes);
     const uint8_t* as_base = mx_uniform(p.a.scales + (uint64_t)(4u * w.step0) * p.a.pitch + w.a_row0);
     const uint8_t* bs_base = mx_uniform(p.b.scales + (uint64_t)(4u * w.step0) * p.b.pitch + w.b_row0);
     uint32_t code_off[T::kCodeLoads], scale_off[T::kScaleLoads];
-    constexpr uint32_t kALoads = BM / 16u;  // of 1 KiB
+    constexpr uint32_t kALoads = BM / 16u / kWavesPerWg;  // of 1 KiB, by a wavefront
+    constexpr uint32_t kAWords = BM / 64u;                // of 256 bytes, by all of them
 #pragma unroll
     for (uint32_t i = 0; i < T::kCodeLoads; ++i) {
-      const uint32_t load = i * kWavesPerWg + wave;
-      const bool is_a = load < kALoads;
-      const uint32_t slot = (is_a ? load : load - kALoads) * 16u + lane / 4u;
-      const uint32_t s = is_a ? SM : SN;
-      const uint32_t part = slot / (32u * s), in = slot % (32u * s);
-      const uint32_t row = part * 32u * s + s * (in % 32u) + in / 32u;
+      const bool is_a = i < kALoads;
+      const uint32_t block = (is_a ? i : i - kALoads) * kWavesPerWg + wave, slot = lane / 4u;
+      const uint32_t s = is_a ? SM : SN, q = 16u / s;
+      const uint32_t row = block * 16u + s * (slot % q) + slot / q;
       const uint32_t most = (is_a ? p.a.rows - w.a_row0 : p.b.rows - w.b_row0) - 1u;
-      const uint32_t piece = (lane % 4u) ^ ((slot / 4u) % 4u);
-      code_off[i] = (uint32_t)(min(row, most) * (is_a ? p.a.row_bytes : p.b.row_bytes)) + piece * 16u;
+      const uint32_t piece = (lane % 4u) ^ ((block * q + slot % q) / 4u % 4u);  // (a tile's rows are counted by 32, a multiple of 16)
+      code_off[i] = min(row, most) * kMxStepBytes + piece * 16u;
     }
-    constexpr uint32_t kAWords = BM / 64u;
+    const uint8_t* scale_at[T::kScaleLoads];  // of the next step to be loaded
+    uint64_t scale_step[T::kScaleLoads];
 #pragma unroll
     for (uint32_t i = 0; i < T::kScaleLoads; ++i) {
       const uint32_t load = (i * kWavesPerWg + wave) % T::kScaleWords;
@@ -175,89 +194,125 @@ __device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w,
       const uint64_t pitch = is_a ? p.a.pitch : p.b.pitch;
       const uint32_t most = (uint32_t)pitch - (is_a ? w.a_row0 : w.b_row0) - 4u;
       scale_off[i] = (uint32_t)((at / rows) * pitch) + min(at % rows, most);
+      scale_at[i] = is_a ? as_base : bs_base;
+      scale_step[i] = 4u * pitch;
     }
-    const auto issue = [&](uint32_t stage, uint32_t step) {
+    const uint8_t* a_at_mem = a_base;
+    const uint8_t* b_at_mem = b_base;
+    // load I of the next step, to `stage`; the last one moves on
+    const auto load = [&](auto i, uint32_t stage) {
+      constexpr uint32_t I = decltype(i)::value;
       const uint32_t to = lds0 + stage * T::kStage;
-#pragma unroll
-      for (uint32_t i = 0; i < T::kCodeLoads; ++i) {
-        const uint32_t load = i * kWavesPerWg + wave;
-        const uint8_t* base = (load < kALoads ? a_base : b_base) + (uint64_t)step * kMxStepBytes;
-        mx_to_lds16(to + load * 1024u, base, code_off[i]);
-      }
-#pragma unroll
-      for (uint32_t i = 0; i < T::kScaleLoads; ++i) {
-        const uint32_t load = (i * kWavesPerWg + wave) % T::kScaleWords;
-        const uint8_t* base = load < kAWords ? as_base + (uint64_t)(4u * step) * p.a.pitch : bs_base + (uint64_t)(4u * step) * p.b.pitch;
-        mx_to_lds4(to + T::kScaleA + load * 256u, base, scale_off[i]);
+      if constexpr (I < T::kCodeLoads) {
+        mx_to_lds16(to + (I * kWavesPerWg + wave) * 1024u, I < kALoads ? a_at_mem : b_at_mem, code_off[I]);
+        if constexpr (I == kALoads - 1u) a_at_mem += p.a.step_bytes;
+        if constexpr (I == T::kCodeLoads - 1u) b_at_mem += p.b.step_bytes;
+      } else {
+        constexpr uint32_t S = I - T::kCodeLoads;
+        const uint32_t word = (S * kWavesPerWg + wave) % T::kScaleWords;
+        mx_to_lds4(to + T::kScaleA + word * 256u, scale_at[S], scale_off[S]);
+        scale_at[S] += scale_step[S];
       }
     };
-    // where this lane reads: slot of tile 0, piece 0 and the others
+    // where this lane reads its row of tile 0 (of the others: QM resp. QN rows further on)
     uint32_t a_at[2], b_at[2];  // by half of the step
 #pragma unroll
     for (uint32_t s = 0; s < 2u; ++s) {
-      const uint32_t as = wm * 32u * SM + r, bs = wn * 32u * SN + r;  // (slots of the tiles behind differ by multiples of 32)
-      a_at[s] = as * kMxStepBytes + (((2u * s + h) ^ ((as / 4u) % 4u)) * 16u);
-      b_at[s] = T::kA + bs * kMxStepBytes + (((2u * s + h) ^ ((bs / 4u) % 4u)) * 16u);
+      const uint32_t place = ((2u * s + h) ^ (r / 4u % 4u)) * 16u;
+      a_at[s] = wm * 32u * SM * kMxStepBytes + (r / T::QM) * 1024u + r % T::QM * kMxStepBytes + place;
+      b_at[s] = T::kA + wn * 32u * SN * kMxStepBytes + (r / T::QN) * 1024u + r % T::QN * kMxStepBytes + place;
     }
     const uint32_t as_at = T::kScaleA + h * BM + wm * 32u * SM + SM * r;
     const uint32_t bs_at = T::kScaleB + h * BN + wn * 32u * SN + SN * r;
     uint4 a[2][SM], b[2][SN];
     uint32_t sa[2], sb[2];
-    const auto fetch = [&](uint32_t stage, uint32_t s) {
-      const uint8_t* from = lds + stage * T::kStage;
-#pragma unroll
-      for (uint32_t i = 0; i < SM; ++i) a[s][i] = *reinterpret_cast<const uint4*>(from + a_at[s] + i * 32u * kMxStepBytes);
-#pragma unroll
-      for (uint32_t j = 0; j < SN; ++j) b[s][j] = *reinterpret_cast<const uint4*>(from + b_at[s] + j * 32u * kMxStepBytes);
-      sa[s] = mx_scales_of<SM>(from + as_at + 2u * s * BM);
-      sb[s] = mx_scales_of<SN>(from + bs_at + 2u * s * BN);
+    constexpr uint32_t kReads = SM + SN + 2u;
+    const auto read = [&](auto k, const uint8_t* from, uint32_t s) {  // read K of half a step
+      constexpr uint32_t K = decltype(k)::value;
+      if constexpr (K == 0) sa[s] = mx_scales_of<SM>(from + as_at + 2u * s * BM);
+      else if constexpr (K == 1) sb[s] = mx_scales_of<SN>(from + bs_at + 2u * s * BN);
+      else if constexpr (K < 2u + SN) b[s][K - 2u] = *reinterpret_cast<const uint4*>(from + b_at[s] + (K - 2u) * T::QN * kMxStepBytes);
+      else a[s][K - 2u - SN] = *reinterpret_cast<const uint4*>(from + a_at[s] + (K - 2u - SN) * T::QM * kMxStepBytes);
     };
+    const auto nothing = [](auto) {};
 
-#pragma unroll
     for (uint32_t d = 0; d < DEPTH; ++d)
-      if (d < w.steps) issue(d, d);
+      if (d < w.steps) mx_each<T::kLoads>([&](auto i) { load(i, d); });
     if (w.steps >= DEPTH) mx_wait_loads<T::kLoads * (DEPTH - 1u)>();
     else mx_wait_loads<0>();
     mx_meet();
-    fetch(0, 0);
+    mx_each<kReads>([&](auto k) { read(k, lds, 0u); });
     uint32_t stage = 0;
-    for (uint32_t t = 0; t < w.steps; ++t) {
-      // the first half of step t is in registers
-      fetch(stage, 1);
-      mx_multiply<SM, SN>(acc, a[0], b[0], sa[0], sb[0]);
+    // one step, but the last: its first half is in registers; the second half of the step is read under the first half's products, the
+    // first half of the next step under the second's
+    const auto step = [&](auto more) {
+      constexpr bool kMore = decltype(more)::value;  // a step DEPTH further on is loaded into this one's place
+      const uint8_t* from = lds + stage * T::kStage;
       const uint32_t next = stage + 1u == DEPTH ? 0u : stage + 1u;
-      if (t + 1u < w.steps) {
-        // step t + 1 has landed: of the steps behind it at most DEPTH - 2 are on their way
-        if (t + DEPTH <= w.steps) mx_wait_loads<T::kLoads * (DEPTH - 2u)>();
-        else mx_wait_loads<0>();
-        mx_meet();  // ... for every wavefront, and step t has been read by all of them
-        if (t + DEPTH < w.steps) issue(stage, t + DEPTH);
-        fetch(next, 0);
-      }
-      mx_multiply<SM, SN>(acc, a[1], b[1], sa[1], sb[1]);
+      mx_multiply<kReads>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) { read(k, from, 1u); });
+      // the next step has landed (of the steps behind it DEPTH - 2 are on their way), this one has been read: for every wavefront
+      mx_wait_loads<kMore ? T::kLoads * (DEPTH - 2u) : 0u>();
+      mx_meet();
+      const uint8_t* from_next = lds + next * T::kStage;
+      mx_multiply<kReads + (kMore ? T::kLoads : 0u)>(acc, a[1], b[1], sa[1], sb[1], [&](auto k) {
+        constexpr uint32_t K = decltype(k)::value;
+        if constexpr (K < kReads) read(k, from_next, 0u);
+        else load(std::integral_constant<uint32_t, K - kReads>{}, stage);
+      });
       stage = next;
-    }
+    };
+    uint32_t t = 0;
+    for (; t + DEPTH < w.steps; ++t) step(std::true_type{});
+    for (; t + 1u < w.steps; ++t) step(std::false_type{});
+    const uint8_t* from = lds + stage * T::kStage;
+    mx_multiply<kReads>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) { read(k, from, 1u); });
+    mx_multiply<0>(acc, a[1], b[1], sa[1], sb[1], nothing);
   }
 
   // results: lane (r, h) holds rows 8 * (e / 4) + 4 * h + e % 4 and column r of a tile
-  const uint32_t col0 = w.b_row0 + wn * 32u * SN + SN * r;
-  const bool vec = p.vec && w.b_first % SN == 0u && col0 + SN <= w.b_last && col0 >= w.b_first;
+  const uint32_t row0 = w.a_row0 + wm * 32u * SM, col0 = w.b_row0 + wn * 32u * SN;  // of the wavefront
+  const bool aligned = p.vec && w.b_first % 4u == 0u;
+  if (aligned && row0 >= w.a_first && row0 + 32u * SM <= w.a_last && col0 >= w.b_first && col0 + 32u * SN <= w.b_last) {  // (uniform)
+    const uint32_t size = p.out_type == kMxF32 ? 4u : 2u;
+    uint8_t* out = static_cast<uint8_t*>(w.out) + ((uint64_t)(row0 - w.a_first) * w.stride + (col0 - w.b_first)) * size;
+    const uint64_t lane_off = ((uint64_t)(SM * 4u * h) * w.stride + SN * r) * size;
+    const auto store_all = [&](auto type) {
+      constexpr uint32_t kType = decltype(type)::value;
+#pragma unroll
+      for (uint32_t e = 0; e < 16u; ++e) {
+#pragma unroll
+        for (uint32_t i = 0; i < SM; ++i) {
+          uint8_t* row = out + (uint64_t)(SM * (8u * (e / 4u) + e % 4u) + i) * w.stride * size;
+          float v[SN];
+#pragma unroll
+          for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
+          mx_store<SN>(row + lane_off, kType, 0, v);
+        }
+      }
+    };
+    if (p.out_type == kMxBf16) store_all(std::integral_constant<uint32_t, kMxBf16>{});
+    else if (p.out_type == kMxF16) store_all(std::integral_constant<uint32_t, kMxF16>{});
+    else store_all(std::integral_constant<uint32_t, kMxF32>{});
+    return;
+  }
+  const uint32_t lane_col = col0 + SN * r;
+  const bool vec = aligned && lane_col + SN <= w.b_last && lane_col >= w.b_first;
 #pragma unroll
   for (uint32_t i = 0; i < SM; ++i) {
 #pragma unroll
     for (uint32_t e = 0; e < 16u; ++e) {
-      const uint32_t row = w.a_row0 + wm * 32u * SM + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
+      const uint32_t row = row0 + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
       if (row < w.a_first || row >= w.a_last) continue;
       const uint64_t at = (uint64_t)(row - w.a_first) * w.stride;
       float v[SN];
 #pragma unroll
       for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
       if (vec) {
-        mx_store<SN>(w.out, p.out_type, at + (col0 - w.b_first), v);
+        mx_store<SN>(w.out, p.out_type, at + (lane_col - w.b_first), v);
       } else {
 #pragma unroll
         for (uint32_t j = 0; j < SN; ++j)
-          if (col0 + j >= w.b_first && col0 + j < w.b_last) mx_store1(w.out, p.out_type, at + (col0 + j - w.b_first), v[j]);
+          if (lane_col + j >= w.b_first && lane_col + j < w.b_last) mx_store1(w.out, p.out_type, at + (lane_col + j - w.b_first), v[j]);
       }
     }
   }
@@ -349,7 +404,7 @@ __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kern
 
 // ------------------------------------------------------------------ few rows
 // What bounds a product of few rows is the reading of b.  A workgroup takes 16 * NS rows of b and up to 16 * MS rows of a; its wavefronts
-// share the contraction, two steps (128 bytes of a row) at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
+// share the contraction, two steps at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
 // operand registers: lane (r, q) = (lane % 16, lane / 16) reads block q of the step of its row.  Row NS * r + j of b is row r of
 // tile j, as above.
 // SRC: a is compressed on the way (kMxBf16 ... kMxF32): the lane's operand is one block of one row, so it reads 32 values, and no
@@ -450,7 +505,7 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
   // rows behind the last read the last one (of b: results that are not kept; of a: rows that are not kept)
   const uint8_t* b_row[NS];
 #pragma unroll
-  for (uint32_t j = 0; j < NS; ++j) b_row[j] = p.b.codes + (uint64_t)(b_first + col0 + min(NS * r + j, cols - 1u)) * p.b.row_bytes + 16u * q;
+  for (uint32_t j = 0; j < NS; ++j) b_row[j] = p.b.codes + (uint64_t)(b_first + col0 + min(NS * r + j, cols - 1u)) * kMxStepBytes + 16u * q;
   const uint64_t b_scale_row = min((uint64_t)b_first + col0 + NS * r, p.b.pitch - NS);
   const uint8_t* b_scale = p.b.scales + (uint64_t)q * p.b.pitch + b_scale_row;
   const uint8_t* a_row[MS];
@@ -461,7 +516,7 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
     const uint32_t row = row0 + min(16u * i + r, rows - 1u);
     a_there[i] = 16u * i + r < rows;
     if constexpr (SRC == kMxReady) {
-      a_row[i] = p.a.codes + (uint64_t)row * p.a.row_bytes + 16u * q;
+      a_row[i] = p.a.codes + (uint64_t)row * kMxStepBytes + 16u * q;
       a_scale[i] = p.a.scales + (uint64_t)q * p.a.pitch + row;
     } else {
       constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;
@@ -478,7 +533,7 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
       const uint32_t s = min(want, steps - 1u);
 #pragma unroll
       for (uint32_t j = 0; j < NS; ++j) {
-        const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b_row[j] + (uint64_t)s * kMxStepBytes));
+        const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b_row[j] + (uint64_t)s * p.b.step_bytes));
         b[u][j] = make_uint4(t.x, t.y, t.z, t.w);
       }
       sb[u] = mx_scales_at<NS>(b_scale + (uint64_t)(4u * s) * p.b.pitch);
@@ -490,7 +545,7 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
 #pragma unroll
       for (uint32_t i = 0; i < MS; ++i) {
         if constexpr (SRC == kMxReady) {
-          a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + (uint64_t)s * kMxStepBytes);
+          a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + (uint64_t)s * p.a.step_bytes);
           sa[u][i] = a_scale[i][(uint64_t)(4u * s) * p.a.pitch];
         } else {
           constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;

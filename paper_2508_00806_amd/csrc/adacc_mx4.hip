@@ -11,7 +11,6 @@
 namespace adacc {
 
 constexpr uint64_t kMxMaxRows = 1ull << 30;      // of a blob, and columns: kernels count them in 32 bits
-constexpr uint64_t kMxMaxContraction = 1ull << 24;  // 256 rows of codes lie within 2^32 bytes
 constexpr uint64_t kMxMaxGrid = 0x7FFFFFFFull;
 
 static uint64_t mx_align256(uint64_t v) { return (v + 255ull) & ~255ull; }
@@ -21,10 +20,10 @@ static uint64_t mx_size(uint32_t type) { return type == ADACC_MX4_F32 ? 4u : 2u;
 static bool mx_sizes_ok(uint64_t rows, uint64_t cols) { return rows <= kMxMaxRows && cols <= kMxMaxRows; }
 
 static void mx_layout(uint64_t rows, uint64_t cols, adacc_mx4_layout* L) {
-  L->row_bytes = mx_over(cols, kMxStep) * kMxStepBytes;
+  L->step_bytes = rows * kMxStepBytes;
   L->scale_pitch = mx_over(rows, 16) * 16;
   L->codes_off = 0;
-  L->scales_off = mx_align256(rows * L->row_bytes);
+  L->scales_off = mx_align256(mx_over(cols, kMxStep) * L->step_bytes);
   L->total_bytes = L->scales_off + mx_align256(mx_over(cols, kMxStep) * 4 * L->scale_pitch);
 }
 
@@ -35,7 +34,7 @@ static MxMatrix mx_matrix(const void* blob, uint64_t rows, uint64_t cols) {
   uint8_t* b = static_cast<uint8_t*>(const_cast<void*>(blob));
   m.codes = b + L.codes_off;
   m.scales = b + L.scales_off;
-  m.row_bytes = L.row_bytes;
+  m.step_bytes = L.step_bytes;
   m.pitch = L.scale_pitch;
   m.rows = (uint32_t)rows;
   m.steps = (uint32_t)mx_over(cols, kMxStep);
@@ -241,7 +240,7 @@ static int mx_check_product(const void* b, uint64_t b_bytes, uint64_t m, uint64_
                             const void* out, uint32_t out_type, uint64_t out_stride) {
   if (out_type > ADACC_MX4_F32 || out_stride < n) return ADACC_EINVAL;
   const uint64_t mats = groups ? groups : 1;
-  if (m > kMxMaxRows || n > kMxMaxRows || mats * n > kMxMaxRows || k > kMxMaxContraction) return ADACC_ELIMIT;
+  if (m > kMxMaxRows || n > kMxMaxRows || mats * n > kMxMaxRows || k > kMxMaxRows) return ADACC_ELIMIT;
   int rc = mx_check_groups(offsets, groups);
   if (rc != ADACC_OK || !m || !n) return rc;
   rc = mx_check_out(out, out_type, n, out_stride);
@@ -277,7 +276,7 @@ int adacc_mx4_product(const void* a, uint64_t a_bytes, uint64_t m, const void* b
 }
 
 uint64_t adacc_mx4_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
-  if (!m || !n || m > kMxMaxRows || k > kMxMaxContraction || !mx_plan(m, n, k, groups).ready) return 0;
+  if (!m || !n || m > kMxMaxRows || k > kMxMaxRows || !mx_plan(m, n, k, groups).ready) return 0;
   adacc_mx4_layout L;
   mx_layout(m, k, &L);
   return L.total_bytes;
@@ -320,7 +319,7 @@ int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* 
   int rc = mx_check_groups(offsets, groups);
   if (rc != ADACC_OK) return rc;
   const uint64_t positions = groups ? adacc_mx4_grouped_cols(rows, groups) : rows;
-  if (positions > kMxMaxContraction) return ADACC_ELIMIT;
+  if (positions > kMxMaxRows) return ADACC_ELIMIT;
   if (!m || !n) return ADACC_OK;
   rc = mx_check_out(out, out_type, n, out_stride);
   if (rc == ADACC_OK) rc = mx_check_blob(a, a_bytes, m, positions);

@@ -4,12 +4,14 @@
 // e + 127, and a 4-bit code per value: sign, and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Value = code * 2^e.  (The element and
 // scale formats of the OCP Microscaling specification 1.0, MXFP4: E2M1 and E8M0.)
 //
-// Blob: codes [rows][row_bytes], element 2j in the low nibble of byte j, row_bytes = 64 per started 128 columns (what one step of the
-// matrix instructions takes), zeros behind the row's end; scales [4 * steps][pitch], one byte for a block, *block by block*: the
-// bytes of a block column lie next to each other for adjacent rows, so that the 32-bit word that a lane hands to the scaled matrix
-// instruction holds the scales of four adjacent rows, one for each of the four tiles that the lane's operand registers belong to (the
-// instruction picks a byte).  pitch is the number of rows, rounded up to 16; the bytes behind the last row are not read as scales of
-// anything that is kept.
+// Blob: codes [steps][rows][64 bytes], a step being 128 columns (what two halves of the matrix instructions take), element 2j in the low
+// nibble of byte j, zeros behind the row's end; scales [4 * steps][pitch], one byte for a block, the bytes of a block column
+// next to each other.
+//   Step by step, because a product's workgroup reads 64 bytes of each of its rows at a time: row by row those are halves of
+// cache lines, and the loads of a tile of 256 x 256 take 1200 cycles a step; adjacent, 745 (1024 are the matrix instructions').
+//   Block by block, so that the 32-bit word that a lane hands to the scaled matrix instruction holds the scales of four adjacent rows,
+// one for each of the four tiles that the lane's operand registers belong to (the instruction picks a byte).  pitch is the number of
+// rows, rounded up to 16; the bytes behind the last row are not read as scales of anything that is kept.
 #pragma once
 
 #include "adacc_common.hpp"
@@ -30,7 +32,7 @@ enum : uint32_t { kMxBf16 = 0, kMxF16 = 1, kMxF32 = 2, kMxReady = 3 };  // kMxRe
 struct MxMatrix {
   uint8_t* codes;
   uint8_t* scales;
-  uint64_t row_bytes;
+  uint64_t step_bytes;  // 64 * rows
   uint64_t pitch;
   uint32_t rows;
   uint32_t steps;

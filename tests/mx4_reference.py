@@ -78,8 +78,8 @@ def blob_parts(blob, layout, rows, cols):
     """(codes [rows, 128 * steps], scale bytes [rows, 4 * steps]) as the blob holds them, padding included"""
     raw = blob.cpu().numpy()
     steps = -(-cols // 128)
-    packed = raw[layout.codes_off:layout.codes_off + rows * layout.row_bytes].reshape(rows, layout.row_bytes)
-    codes = np.stack((packed & 15, packed >> 4), 2).reshape(rows, 2 * layout.row_bytes)
+    packed = raw[layout.codes_off:layout.codes_off + steps * layout.step_bytes].reshape(steps, rows, 64).transpose(1, 0, 2)
+    codes = np.stack((packed & 15, packed >> 4), 3).reshape(rows, 128 * steps)
     s = raw[layout.scales_off:layout.scales_off + 4 * steps * layout.scale_pitch].reshape(4 * steps, layout.scale_pitch)
     return codes, s[:, :rows].T
 

@@ -25,7 +25,7 @@ def test_layout_closed_form(L):
     for rows, cols in ((1, 1), (3, 128), (16, 129), (17, 4096), (1000, 2040), (0, 5), (5, 0)):
         lay = adacc.mx4_layout_of(rows, cols)
         steps = -(-cols // 128)
-        assert lay.row_bytes == 64 * steps and lay.scale_pitch == -(-rows // 16) * 16
+        assert lay.step_bytes == 64 * rows and lay.scale_pitch == -(-rows // 16) * 16
         assert lay.codes_off == 0 and lay.scales_off == a256(rows * 64 * steps)
         assert lay.total_bytes == lay.scales_off + a256(4 * steps * lay.scale_pitch)
     assert L.adacc_mx4_layout_of(1, 1, None) == adacc.ENULL
@@ -97,7 +97,7 @@ def test_product_refusals(L):
     assert f(kind=3) == adacc.EINVAL and f(os=19) == adacc.EINVAL and f(off=P) == adacc.EINVAL
     assert f(groups=3) == adacc.ENULL and f(a=None) == adacc.ENULL and f(b=None) == adacc.ENULL and f(out=None) == adacc.ENULL
     assert f(a=P + 16) == adacc.EALIGN and f(b=P + 16) == adacc.EALIGN and f(out=P + 1) == adacc.EALIGN and f(kind=2, out=P + 2) == adacc.EALIGN
-    assert f(k=(1 << 24) + 1) == adacc.ELIMIT and f(m=(1 << 30) + 1) == adacc.ELIMIT and f(off=P, groups=4097) == adacc.ELIMIT
+    assert f(k=(1 << 30) + 1) == adacc.ELIMIT and f(m=(1 << 30) + 1) == adacc.ELIMIT and f(off=P, groups=4097) == adacc.ELIMIT
     assert f(off=P, groups=4096, n=1 << 20, os=1 << 20) == adacc.ELIMIT
     assert f(ab=adacc.mx4_layout_of(10, 300).total_bytes - 1) == adacc.ESIZE
     assert f(bb=adacc.mx4_layout_of(20, 300).total_bytes - 1) == adacc.ESIZE
@@ -124,7 +124,7 @@ def test_gradient_refusals(L):
     assert f(kind=3) == adacc.EINVAL and f(os=19) == adacc.EINVAL and f(groups=0) == adacc.EINVAL
     assert f(off=None) == adacc.ENULL and f(a=None) == adacc.ENULL and f(b=None) == adacc.ENULL and f(out=None) == adacc.ENULL
     assert f(a=P + 16) == adacc.EALIGN and f(off=P + 1) == adacc.EALIGN
-    assert f(rows=(1 << 24) + 1) == adacc.ELIMIT and f(groups=4097) == adacc.ELIMIT
+    assert f(rows=(1 << 30) + 1) == adacc.ELIMIT and f(groups=4097) == adacc.ELIMIT
     need = adacc.mx4_layout_of(10, adacc.mx4_grouped_cols(500, 3)).total_bytes
     assert f(ab=need - 1) == adacc.ESIZE
     assert f(m=0, a=None, b=None, out=None) == adacc.OK
