@@ -648,26 +648,36 @@ def mx4_grouped_cols(rows: int, groups: int) -> int:
     return int(lib().adacc_mx4_grouped_cols(rows, groups))
 
 
+_mx4_types = {}
+
+
 def _mx4_type(t):
-    import torch
-    try:
-        return {torch.bfloat16: MX4_BF16, torch.float16: MX4_F16, torch.float32: MX4_F32}[t.dtype]
-    except KeyError:
-        raise TypeError(f"bfloat16, float16 or float32 is needed, not {t.dtype}") from None
+    kind = _mx4_types.get(t.dtype)
+    if kind is None:
+        if not _mx4_types:
+            import torch
+            _mx4_types.update({torch.bfloat16: MX4_BF16, torch.float16: MX4_F16, torch.float32: MX4_F32})
+            return _mx4_type(t)
+        raise TypeError(f"bfloat16, float16 or float32 is needed, not {t.dtype}")
+    return kind
 
 
 def _mx4_rows(t, what):
     """The stride between the rows of a matrix whose rows lie in one piece each."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must be a matrix with adjacent columns")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be a matrix")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must have adjacent columns")
+    return stride if rows > 1 else cols
 
 
 def _mx4_groups(offsets):
     """(device pointer, number of groups) of an int32 tensor of groups + 1 offsets, or of None."""
-    import torch
     if offsets is None:
         return None, 0
+    import torch
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.numel() < 2:
         raise TypeError("offsets must be a contiguous int32 tensor of one offset more than there are groups")
     return offsets.data_ptr(), offsets.numel() - 1
@@ -707,7 +717,7 @@ def mx4_product(a, b, k: int, out, offsets=None, stream=None):
     stride = _mx4_rows(out, "out")
     off, groups = _mx4_groups(offsets)
     m, n = out.shape
-    _check(lib().adacc_mx4_product(*_mx4_blob(a), m, *_mx4_blob(b), n, k, off, groups, _ptr(out), kind, max(stride, n), _stream(stream)),
+    _check(lib().adacc_mx4_product(*_mx4_blob(a), m, *_mx4_blob(b), n, k, off, groups, _ptr(out), kind, stride, _stream(stream)),
            "adacc_mx4_product")
 
 
@@ -725,8 +735,8 @@ def mx4_linear(x, b, out, offsets=None, workspace=None, scale_rule=MX4_SCALE_FLO
     n = out.shape[1]
     if out.shape[0] != m:
         raise ValueError(f"out has {out.shape[0]} rows, x has {m}")
-    _check(lib().adacc_mx4_linear(kind, scale_rule, _ptr(x), m, max(x_stride, k), *_mx4_blob(b), n, k, off, groups, _ptr(out), okind,
-                                  max(o_stride, n), *_mx4_blob(workspace), _stream(stream)), "adacc_mx4_linear")
+    _check(lib().adacc_mx4_linear(kind, scale_rule, _ptr(x), m, x_stride, *_mx4_blob(b), n, k, off, groups, _ptr(out), okind, o_stride,
+                                  *_mx4_blob(workspace), _stream(stream)), "adacc_mx4_linear")
 
 
 def mx4_gradient(a, b, rows: int, out, offsets=None, stream=None):
@@ -745,7 +755,7 @@ def alloc_mx4(rows: int, cols: int, device="cuda"):
     """(blob, layout) for a matrix [rows, cols]."""
     import torch
     L = mx4_layout_of(rows, cols)
-    return torch.empty(int(L.total_bytes), dtype=torch.uint8, device=device), L
+    return torch.empty(L.total_bytes, dtype=torch.uint8, device=device), L
 
 
 # ---------------------------------------------------------------- buffer helpers (allocation = plumbing)

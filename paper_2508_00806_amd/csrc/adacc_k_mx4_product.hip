@@ -114,6 +114,8 @@ template <uint32_t I, uint32_t J>
 __device__ __forceinline__ mx_f16v mx_mfma32(uint4 a, uint4 b, mx_f16v c, uint32_t sa, uint32_t sb) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(a), mx_operand(b), c, kMxFp4, kMxFp4, I, (int)sa, J, (int)sb);
 }
+constexpr uint32_t mx_least(uint32_t a, uint32_t b) { return a < b ? a : b; }
+
 // f(0), f(1), ... f(N - 1), with constants
 template <uint32_t N, typename F, uint32_t... I>
 __device__ __forceinline__ void mx_each(F&& f, std::integer_sequence<uint32_t, I...>) {
@@ -131,7 +133,8 @@ __device__ __forceinline__ void mx_multiply(mx_f16v (&acc)[SM][SN], const uint4 
   mx_each<SM * SN>([&](auto q) {
     constexpr uint32_t Q = decltype(q)::value, I = Q / SN, J = Q % SN;
     acc[I][J] = mx_mfma32<I, J>(a[I], b[J], acc[I][J], sa, sb);
-    constexpr uint32_t kFrom = Q * TASKS / (SM * SN), kTo = (Q + 1u) * TASKS / (SM * SN);
+    constexpr uint32_t kEach = (TASKS + SM * SN - 1u) / (SM * SN);  // tasks come early: what they read has the rest of the half step to arrive
+    constexpr uint32_t kFrom = Q * kEach < TASKS ? Q * kEach : TASKS, kTo = (Q + 1u) * kEach < TASKS ? (Q + 1u) * kEach : TASKS;
     mx_each<kTo - kFrom>([&](auto k) { task(std::integral_constant<uint32_t, kFrom + decltype(k)::value>{}); });
     __builtin_amdgcn_sched_barrier(0);
   });
@@ -147,8 +150,10 @@ struct MxWork {
   uint64_t stride;
 };
 
-template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
-__device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w, uint8_t* lds) {
+// The workgroup's tiles, one after the other: next(&work) gives the next one, or false.  The first loads of a tile are on their way while the
+// results of the one before are written.
+template <uint32_t BM, uint32_t BN, uint32_t DEPTH, typename Next>
+__device__ __forceinline__ void mx_tiles(const MxProductArgs& p, uint8_t* lds, Next&& next_work) {
   using T = MxTile<BM, BN, DEPTH>;
   constexpr uint32_t SM = T::SM, SN = T::SN;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -156,23 +161,18 @@ __device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w,
   const uint32_t r = lane % 32u, h = lane / 32u;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(mx_lds_address(lds));
 
-  mx_f16v acc[SM][SN];
-#pragma unroll
-  for (uint32_t i = 0; i < SM; ++i)
-#pragma unroll
-    for (uint32_t j = 0; j < SN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < 16u; ++e) acc[i][j][e] = 0.0f;
-
-  if (w.steps) {  // (uniform in the workgroup)
-    // what this wavefront loads of every step.  Rows behind the matrix's last read the last one: the results are not kept.
-    const uint8_t* a_base = mx_uniform(p.a.codes + (uint64_t)w.step0 * p.a.step_bytes + (uint64_t)w.a_row0 * kMxStepBytes);
-    const uint8_t* b_base = mx_uniform(p.b.codes + (uint64_t)w.step0 * p.b.step_bytes + (uint64_t)w.b_row0 * kMxStepBytes);
-    const uint8_t* as_base = mx_uniform(p.a.scales + (uint64_t)(4u * w.step0) * p.a.pitch + w.a_row0);
-    const uint8_t* bs_base = mx_uniform(p.b.scales + (uint64_t)(4u * w.step0) * p.b.pitch + w.b_row0);
-    uint32_t code_off[T::kCodeLoads], scale_off[T::kScaleLoads];
-    constexpr uint32_t kALoads = BM / 16u / kWavesPerWg;  // of 1 KiB, by a wavefront
-    constexpr uint32_t kAWords = BM / 64u;                // of 256 bytes, by all of them
+  // ---- what this wavefront loads of every step
+  constexpr uint32_t kALoads = BM / 16u / kWavesPerWg;  // of 1 KiB, by a wavefront
+  constexpr uint32_t kAWords = BM / 64u;                // of 256 bytes, by all of them
+  const uint8_t* a_mem;  // of the next step to be loaded
+  const uint8_t* b_mem;
+  const uint8_t* scale_mem[T::kScaleLoads];
+  uint64_t scale_step[T::kScaleLoads];
+  uint32_t code_off[T::kCodeLoads], scale_off[T::kScaleLoads];
+  // Rows behind the matrix's last read the last one: the results are not kept.
+  const auto aim = [&](const MxWork& w) {
+    a_mem = mx_uniform(p.a.codes + (uint64_t)w.step0 * p.a.step_bytes + (uint64_t)w.a_row0 * kMxStepBytes);
+    b_mem = mx_uniform(p.b.codes + (uint64_t)w.step0 * p.b.step_bytes + (uint64_t)w.b_row0 * kMxStepBytes);
 #pragma unroll
     for (uint32_t i = 0; i < T::kCodeLoads; ++i) {
       const bool is_a = i < kALoads;
@@ -183,8 +183,6 @@ __device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w,
       const uint32_t piece = (lane % 4u) ^ ((block * q + slot % q) / 4u % 4u);  // (a tile's rows are counted by 32, a multiple of 16)
       code_off[i] = min(row, most) * kMxStepBytes + piece * 16u;
     }
-    const uint8_t* scale_at[T::kScaleLoads];  // of the next step to be loaded
-    uint64_t scale_step[T::kScaleLoads];
 #pragma unroll
     for (uint32_t i = 0; i < T::kScaleLoads; ++i) {
       const uint32_t load = (i * kWavesPerWg + wave) % T::kScaleWords;
@@ -192,129 +190,182 @@ __device__ __forceinline__ void mx_tile(const MxProductArgs& p, const MxWork& w,
       const uint32_t rows = is_a ? BM : BN;
       const uint32_t at = (is_a ? load : load - kAWords) * 256u + lane * 4u;
       const uint64_t pitch = is_a ? p.a.pitch : p.b.pitch;
-      const uint32_t most = (uint32_t)pitch - (is_a ? w.a_row0 : w.b_row0) - 4u;
-      scale_off[i] = (uint32_t)((at / rows) * pitch) + min(at % rows, most);
-      scale_at[i] = is_a ? as_base : bs_base;
+      const uint32_t row0 = is_a ? w.a_row0 : w.b_row0;
+      scale_off[i] = (uint32_t)((at / rows) * pitch) + min(at % rows, (uint32_t)pitch - row0 - 4u);
+      scale_mem[i] = mx_uniform((is_a ? p.a.scales : p.b.scales) + (uint64_t)(4u * w.step0) * pitch + row0);
       scale_step[i] = 4u * pitch;
     }
-    const uint8_t* a_at_mem = a_base;
-    const uint8_t* b_at_mem = b_base;
-    // load I of the next step, to `stage`; the last one moves on
-    const auto load = [&](auto i, uint32_t stage) {
-      constexpr uint32_t I = decltype(i)::value;
-      const uint32_t to = lds0 + stage * T::kStage;
-      if constexpr (I < T::kCodeLoads) {
-        mx_to_lds16(to + (I * kWavesPerWg + wave) * 1024u, I < kALoads ? a_at_mem : b_at_mem, code_off[I]);
-        if constexpr (I == kALoads - 1u) a_at_mem += p.a.step_bytes;
-        if constexpr (I == T::kCodeLoads - 1u) b_at_mem += p.b.step_bytes;
-      } else {
-        constexpr uint32_t S = I - T::kCodeLoads;
-        const uint32_t word = (S * kWavesPerWg + wave) % T::kScaleWords;
-        mx_to_lds4(to + T::kScaleA + word * 256u, scale_at[S], scale_off[S]);
-        scale_at[S] += scale_step[S];
-      }
-    };
-    // where this lane reads its row of tile 0 (of the others: QM resp. QN rows further on)
-    uint32_t a_at[2], b_at[2];  // by half of the step
-#pragma unroll
-    for (uint32_t s = 0; s < 2u; ++s) {
-      const uint32_t place = ((2u * s + h) ^ (r / 4u % 4u)) * 16u;
-      a_at[s] = wm * 32u * SM * kMxStepBytes + (r / T::QM) * 1024u + r % T::QM * kMxStepBytes + place;
-      b_at[s] = T::kA + wn * 32u * SN * kMxStepBytes + (r / T::QN) * 1024u + r % T::QN * kMxStepBytes + place;
+  };
+  // load I of the next step, to `stage`; the last of a matrix moves on
+  const auto load = [&](auto i, uint32_t stage) {
+    constexpr uint32_t I = decltype(i)::value;
+    const uint32_t to = lds0 + stage * T::kStage;
+    if constexpr (I < T::kCodeLoads) {
+      mx_to_lds16(to + (I * kWavesPerWg + wave) * 1024u, I < kALoads ? a_mem : b_mem, code_off[I]);
+      if constexpr (I == kALoads - 1u) a_mem += p.a.step_bytes;
+      if constexpr (I == T::kCodeLoads - 1u) b_mem += p.b.step_bytes;
+    } else {
+      constexpr uint32_t S = I - T::kCodeLoads;
+      const uint32_t word = (S * kWavesPerWg + wave) % T::kScaleWords;
+      mx_to_lds4(to + T::kScaleA + word * 256u, scale_mem[S], scale_off[S]);
+      scale_mem[S] += scale_step[S];
     }
-    const uint32_t as_at = T::kScaleA + h * BM + wm * 32u * SM + SM * r;
-    const uint32_t bs_at = T::kScaleB + h * BN + wn * 32u * SN + SN * r;
-    uint4 a[2][SM], b[2][SN];
-    uint32_t sa[2], sb[2];
-    constexpr uint32_t kReads = SM + SN + 2u;
-    const auto read = [&](auto k, const uint8_t* from, uint32_t s) {  // read K of half a step
-      constexpr uint32_t K = decltype(k)::value;
-      if constexpr (K == 0) sa[s] = mx_scales_of<SM>(from + as_at + 2u * s * BM);
-      else if constexpr (K == 1) sb[s] = mx_scales_of<SN>(from + bs_at + 2u * s * BN);
-      else if constexpr (K < 2u + SN) b[s][K - 2u] = *reinterpret_cast<const uint4*>(from + b_at[s] + (K - 2u) * T::QN * kMxStepBytes);
-      else a[s][K - 2u - SN] = *reinterpret_cast<const uint4*>(from + a_at[s] + (K - 2u - SN) * T::QM * kMxStepBytes);
-    };
-    const auto nothing = [](auto) {};
+  };
+  // A step's loads go out in two parts, one in either half of the step before last, so that every half has as many tasks
+  constexpr uint32_t kEarly = T::kLoads / 2u;
+  const auto load_early = [&](uint32_t to) { mx_each<kEarly>([&](auto i) { load(i, to); }); };
+  const auto load_rest = [&](uint32_t to) { mx_each<T::kLoads - kEarly>([&](auto i) { load(std::integral_constant<uint32_t, kEarly + decltype(i)::value>{}, to); }); };
+  const auto load_first = [&](uint32_t steps) {
+    for (uint32_t d = 0; d + 1u < DEPTH && d < steps; ++d) {
+      load_early(d);
+      load_rest(d);
+    }
+    if (steps >= DEPTH) load_early(DEPTH - 1u);
+  };
 
-    for (uint32_t d = 0; d < DEPTH; ++d)
-      if (d < w.steps) mx_each<T::kLoads>([&](auto i) { load(i, d); });
-    if (w.steps >= DEPTH) mx_wait_loads<T::kLoads * (DEPTH - 1u)>();
-    else mx_wait_loads<0>();
-    mx_meet();
-    mx_each<kReads>([&](auto k) { read(k, lds, 0u); });
-    uint32_t stage = 0;
-    // one step, but the last: its first half is in registers; the second half of the step is read under the first half's products, the
-    // first half of the next step under the second's
-    const auto step = [&](auto more) {
-      constexpr bool kMore = decltype(more)::value;  // a step DEPTH further on is loaded into this one's place
-      const uint8_t* from = lds + stage * T::kStage;
-      const uint32_t next = stage + 1u == DEPTH ? 0u : stage + 1u;
-      mx_multiply<kReads>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) { read(k, from, 1u); });
-      // the next step has landed (of the steps behind it DEPTH - 2 are on their way), this one has been read: for every wavefront
-      mx_wait_loads<kMore ? T::kLoads * (DEPTH - 2u) : 0u>();
-      mx_meet();
-      const uint8_t* from_next = lds + next * T::kStage;
-      mx_multiply<kReads + (kMore ? T::kLoads : 0u)>(acc, a[1], b[1], sa[1], sb[1], [&](auto k) {
-        constexpr uint32_t K = decltype(k)::value;
-        if constexpr (K < kReads) read(k, from_next, 0u);
-        else load(std::integral_constant<uint32_t, K - kReads>{}, stage);
-      });
-      stage = next;
-    };
-    uint32_t t = 0;
-    for (; t + DEPTH < w.steps; ++t) step(std::true_type{});
-    for (; t + 1u < w.steps; ++t) step(std::false_type{});
-    const uint8_t* from = lds + stage * T::kStage;
-    mx_multiply<kReads>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) { read(k, from, 1u); });
-    mx_multiply<0>(acc, a[1], b[1], sa[1], sb[1], nothing);
+  // ---- where this lane reads its row of tile 0 (of the others: QM resp. QN rows further on)
+  uint32_t a_at[2], b_at[2];  // by half of the step
+#pragma unroll
+  for (uint32_t s = 0; s < 2u; ++s) {
+    const uint32_t place = ((2u * s + h) ^ (r / 4u % 4u)) * 16u;
+    a_at[s] = wm * 32u * SM * kMxStepBytes + (r / T::QM) * 1024u + r % T::QM * kMxStepBytes + place;
+    b_at[s] = T::kA + wn * 32u * SN * kMxStepBytes + (r / T::QN) * 1024u + r % T::QN * kMxStepBytes + place;
   }
+  const uint32_t as_at = T::kScaleA + h * BM + wm * 32u * SM + SM * r;
+  const uint32_t bs_at = T::kScaleB + h * BN + wn * 32u * SN + SN * r;
+  uint4 a[2][SM], b[2][SN];
+  uint32_t sa[2], sb[2];
+  constexpr uint32_t kReads = SM + SN + 2u;
+  const auto read = [&](auto k, const uint8_t* from, uint32_t s) {  // read K of half a step
+    constexpr uint32_t K = decltype(k)::value;
+    if constexpr (K == 0) sa[s] = mx_scales_of<SM>(from + as_at + 2u * s * BM);
+    else if constexpr (K == 1) sb[s] = mx_scales_of<SN>(from + bs_at + 2u * s * BN);
+    else if constexpr (K < 2u + SN) b[s][K - 2u] = *reinterpret_cast<const uint4*>(from + b_at[s] + (K - 2u) * T::QN * kMxStepBytes);
+    else a[s][K - 2u - SN] = *reinterpret_cast<const uint4*>(from + a_at[s] + (K - 2u - SN) * T::QM * kMxStepBytes);
+  };
 
-  // results: lane (r, h) holds rows 8 * (e / 4) + 4 * h + e % 4 and column r of a tile
-  const uint32_t row0 = w.a_row0 + wm * 32u * SM, col0 = w.b_row0 + wn * 32u * SN;  // of the wavefront
-  const bool aligned = p.vec && w.b_first % 4u == 0u;
-  if (aligned && row0 >= w.a_first && row0 + 32u * SM <= w.a_last && col0 >= w.b_first && col0 + 32u * SN <= w.b_last) {  // (uniform)
-    const uint32_t size = p.out_type == kMxF32 ? 4u : 2u;
-    uint8_t* out = static_cast<uint8_t*>(w.out) + ((uint64_t)(row0 - w.a_first) * w.stride + (col0 - w.b_first)) * size;
-    const uint64_t lane_off = ((uint64_t)(SM * 4u * h) * w.stride + SN * r) * size;
-    const auto store_all = [&](auto type) {
-      constexpr uint32_t kType = decltype(type)::value;
+  mx_f16v acc[SM][SN];
+  MxWork w;
+  if (!next_work(w)) return;
+  aim(w);
+  load_first(w.steps);
+  // Stores count as loads do, in order: the kStores of the tile before went out behind this tile's first loads, and what waits for one of those
+  // need not wait for them.  (Where a tile of results was not stored in one piece, their number is not known, and they are waited for.)
+  constexpr uint32_t kStores = 16u * SM;
+  bool behind = false;
+  for (;;) {
+    MxWork following;
+    const bool more = next_work(following);
 #pragma unroll
-      for (uint32_t e = 0; e < 16u; ++e) {
+    for (uint32_t i = 0; i < SM; ++i)
 #pragma unroll
-        for (uint32_t i = 0; i < SM; ++i) {
-          uint8_t* row = out + (uint64_t)(SM * (8u * (e / 4u) + e % 4u) + i) * w.stride * size;
+      for (uint32_t j = 0; j < SN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < 16u; ++e) acc[i][j][e] = 0.0f;
+
+    if (w.steps) {  // (uniform in the workgroup)
+      if (w.steps >= DEPTH) {
+        if (behind) mx_wait_loads<mx_least(T::kLoads * (DEPTH - 2u) + kEarly + kStores, 63u)>();
+        else mx_wait_loads<T::kLoads * (DEPTH - 2u) + kEarly>();
+      } else {
+        mx_wait_loads<0>();
+        behind = false;
+      }
+      mx_meet();
+      mx_each<kReads>([&](auto k) { read(k, lds, 0u); });
+      uint32_t stage = 0, t = 0;
+      // One step, but the last: its first half is in registers; the second half of the step is read under the first half's products, the
+      // first half of the next step under the second's.  REST: the step DEPTH - 1 further on exists, its second part is loaded to where the
+      // step before was; EARLY: so does the one behind it, whose first part is loaded to this step's place.
+      const auto step = [&](auto rest, auto early) {
+        constexpr uint32_t kRest = decltype(rest)::value ? T::kLoads - kEarly : 0u, kFirst = decltype(early)::value ? kEarly : 0u;
+        const uint8_t* from = lds + stage * T::kStage;
+        const uint32_t next = stage + 1u == DEPTH ? 0u : stage + 1u, before = stage == 0u ? DEPTH - 1u : stage - 1u;
+        mx_multiply<kReads + kRest>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) {
+          constexpr uint32_t K = decltype(k)::value;
+          if constexpr (K < kReads) read(k, from, 1u);
+          else load(std::integral_constant<uint32_t, kEarly + K - kReads>{}, before);
+        });
+        // the next step has landed (of those behind it DEPTH - 2 are on their way), this one has been read: for every wavefront
+        if constexpr (kRest) {
+          if (behind && t + 2u < DEPTH) mx_wait_loads<mx_least(T::kLoads * (DEPTH - 2u) + kStores, 63u)>();
+          else mx_wait_loads<T::kLoads * (DEPTH - 2u)>();
+        } else {
+          mx_wait_loads<0>();
+        }
+        mx_meet();
+        const uint8_t* from_next = lds + next * T::kStage;
+        mx_multiply<kReads + kFirst>(acc, a[1], b[1], sa[1], sb[1], [&](auto k) {
+          constexpr uint32_t K = decltype(k)::value;
+          if constexpr (K < kReads) read(k, from_next, 0u);
+          else load(std::integral_constant<uint32_t, K - kReads>{}, stage);
+        });
+        stage = next;
+        ++t;
+      };
+      while (t + DEPTH < w.steps) step(std::true_type{}, std::true_type{});
+      if (t + DEPTH == w.steps) step(std::true_type{}, std::false_type{});
+      while (t + 1u < w.steps) step(std::false_type{}, std::false_type{});
+      const uint8_t* from = lds + stage * T::kStage;
+      mx_multiply<kReads>(acc, a[0], b[0], sa[0], sb[0], [&](auto k) { read(k, from, 1u); });
+      mx_multiply<0>(acc, a[1], b[1], sa[1], sb[1], [](auto) {});
+    }
+    if (more) {
+      mx_meet();  // every wavefront has read its last step
+      aim(following);
+      load_first(following.steps);
+    }
+
+    // results: lane (r, h) holds rows 8 * (e / 4) + 4 * h + e % 4 and column r of a tile
+    const uint32_t row0 = w.a_row0 + wm * 32u * SM, col0 = w.b_row0 + wn * 32u * SN;  // of the wavefront
+    const bool aligned = p.vec && w.b_first % 4u == 0u;
+    behind = aligned && w.stride < (1u << 24) && row0 >= w.a_first && row0 + 32u * SM <= w.a_last && col0 >= w.b_first && col0 + 32u * SN <= w.b_last;  // (uniform)
+    if (behind) {
+      const uint32_t size = p.out_type == kMxF32 ? 4u : 2u;
+      uint8_t* out = static_cast<uint8_t*>(w.out) + ((uint64_t)(row0 - w.a_first) * w.stride + (col0 - w.b_first)) * size;
+      const uint32_t lane_off = (SM * 4u * h * (uint32_t)w.stride + SN * r) * size;  // (below 2^32: uniform addresses and an offset a lane)
+      const auto store_all = [&](auto type) {
+        constexpr uint32_t kType = decltype(type)::value;
+#pragma unroll
+        for (uint32_t e = 0; e < 16u; ++e) {
+#pragma unroll
+          for (uint32_t i = 0; i < SM; ++i) {
+            uint8_t* row = out + (uint64_t)(SM * (8u * (e / 4u) + e % 4u) + i) * w.stride * size;
+            float v[SN];
+#pragma unroll
+            for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
+            mx_store<SN>(row + lane_off, kType, 0, v);
+          }
+        }
+      };
+      if (p.out_type == kMxBf16) store_all(std::integral_constant<uint32_t, kMxBf16>{});
+      else if (p.out_type == kMxF16) store_all(std::integral_constant<uint32_t, kMxF16>{});
+      else store_all(std::integral_constant<uint32_t, kMxF32>{});
+    } else {
+      const uint32_t lane_col = col0 + SN * r;
+      const bool vec = aligned && lane_col + SN <= w.b_last && lane_col >= w.b_first;
+#pragma unroll
+      for (uint32_t i = 0; i < SM; ++i) {
+#pragma unroll
+        for (uint32_t e = 0; e < 16u; ++e) {
+          const uint32_t row = row0 + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
+          if (row < w.a_first || row >= w.a_last) continue;
+          const uint64_t at = (uint64_t)(row - w.a_first) * w.stride;
           float v[SN];
 #pragma unroll
           for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
-          mx_store<SN>(row + lane_off, kType, 0, v);
+          if (vec) {
+            mx_store<SN>(w.out, p.out_type, at + (lane_col - w.b_first), v);
+          } else {
+#pragma unroll
+            for (uint32_t j = 0; j < SN; ++j)
+              if (lane_col + j >= w.b_first && lane_col + j < w.b_last) mx_store1(w.out, p.out_type, at + (lane_col + j - w.b_first), v[j]);
+          }
         }
       }
-    };
-    if (p.out_type == kMxBf16) store_all(std::integral_constant<uint32_t, kMxBf16>{});
-    else if (p.out_type == kMxF16) store_all(std::integral_constant<uint32_t, kMxF16>{});
-    else store_all(std::integral_constant<uint32_t, kMxF32>{});
-    return;
-  }
-  const uint32_t lane_col = col0 + SN * r;
-  const bool vec = aligned && lane_col + SN <= w.b_last && lane_col >= w.b_first;
-#pragma unroll
-  for (uint32_t i = 0; i < SM; ++i) {
-#pragma unroll
-    for (uint32_t e = 0; e < 16u; ++e) {
-      const uint32_t row = row0 + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
-      if (row < w.a_first || row >= w.a_last) continue;
-      const uint64_t at = (uint64_t)(row - w.a_first) * w.stride;
-      float v[SN];
-#pragma unroll
-      for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
-      if (vec) {
-        mx_store<SN>(w.out, p.out_type, at + (lane_col - w.b_first), v);
-      } else {
-#pragma unroll
-        for (uint32_t j = 0; j < SN; ++j)
-          if (lane_col + j >= w.b_first && lane_col + j < w.b_last) mx_store1(w.out, p.out_type, at + (lane_col + j - w.b_first), v[j]);
-      }
     }
+    if (!more) return;
+    w = following;
   }
 }
 
@@ -337,69 +388,79 @@ __device__ __forceinline__ void mx_band(uint32_t id, uint32_t m_tiles, uint32_t 
   *mt = band * kBand + in - *nt * high;
 }
 
+// Workgroups take tiles blockIdx.x, blockIdx.x + gridDim.x, ... (the host launches as many as run at the same time)
 // ---- rows by groups (or one group): a tile row lies within a group
 template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
 __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_product_kernel(MxProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
-  uint32_t mt, nt;
-  mx_band(mx_by_die(blockIdx.x, gridDim.x), p.m_tiles, p.n_tiles, &mt, &nt);
-  const MxPlace at = mx_place<true>(p.g, mt, BM);
-  MxWork w;
-  const uint32_t a_low = at.first & ~3u;
-  if (at.last <= at.first || (uint64_t)at.unit * BM >= (uint64_t)(at.last - a_low)) return;
-  w.a_row0 = a_low + at.unit * BM;
-  w.a_first = at.first;
-  w.a_last = at.last;
-  const bool nobody = at.group >= p.g.groups && p.g.offsets != nullptr;  // rows behind the last group: zeros
-  const uint32_t b_first = nobody ? 0u : at.group * p.n;
-  const uint32_t b_low = b_first & ~3u;
-  w.b_row0 = b_low + nt * BN;
-  w.b_first = b_first;
-  w.b_last = b_first + p.n;
-  if (w.b_row0 >= w.b_last) return;
-  w.step0 = 0;
-  w.steps = nobody ? 0u : p.a.steps;
-  w.out = mx_out_at(p, (uint64_t)at.first * p.out_stride);
-  w.stride = p.out_stride;
-  mx_tile<BM, BN, DEPTH>(p, w, mx_lds);
+  const uint32_t total = p.m_tiles * p.n_tiles;
+  uint32_t id = blockIdx.x;
+  mx_tiles<BM, BN, DEPTH>(p, mx_lds, [&](MxWork& w) {
+    for (; id < total; id += gridDim.x) {
+      uint32_t mt, nt;
+      mx_band(mx_by_die(id, total), p.m_tiles, p.n_tiles, &mt, &nt);
+      const MxPlace at = mx_place<true>(p.g, mt, BM);
+      const uint32_t a_low = at.first & ~3u;
+      if (at.last <= at.first || (uint64_t)at.unit * BM >= (uint64_t)(at.last - a_low)) continue;
+      const bool nobody = at.group >= p.g.groups && p.g.offsets != nullptr;  // rows behind the last group: zeros
+      w.b_first = nobody ? 0u : at.group * p.n;
+      w.b_last = w.b_first + p.n;
+      w.b_row0 = (w.b_first & ~3u) + nt * BN;
+      if (w.b_row0 >= w.b_last) continue;
+      w.a_row0 = a_low + at.unit * BM;
+      w.a_first = at.first;
+      w.a_last = at.last;
+      w.step0 = 0;
+      w.steps = nobody ? 0u : p.a.steps;
+      w.out = mx_out_at(p, (uint64_t)at.first * p.out_stride);
+      w.stride = p.out_stride;
+      id += gridDim.x;
+      return true;
+    }
+    return false;
+  });
 }
 
 // ---- the contraction by groups: out[g] = sum over the group's padded positions
 template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
 __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kernel(MxProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
-  const uint32_t per = p.m_tiles * p.n_tiles;
-  const uint32_t id = mx_by_die(blockIdx.x, gridDim.x);
-  const uint32_t group = id / per;
-  uint32_t mt, nt;
-  mx_band(id - group * per, p.m_tiles, p.n_tiles, &mt, &nt);
-  // steps of the groups before this one, and its own
-  const uint32_t lane = threadIdx.x % kWave;
-  uint32_t before = 0;
-  for (uint32_t g0 = 0; g0 < group; g0 += kWave) {
-    const uint32_t i = g0 + lane;
-    uint32_t steps = 0;
-    if (i < group) {
-      const uint32_t first = mx_offset(p.g, i), last = mx_offset(p.g, i + 1u);
-      steps = last > first ? (last - first + kMxStep - 1u) / kMxStep : 0u;
-    }
+  const uint32_t per = p.m_tiles * p.n_tiles, total = per * p.g.groups;
+  uint32_t id = blockIdx.x;
+  mx_tiles<BM, BN, DEPTH>(p, mx_lds, [&](MxWork& w) {
+    if (id >= total) return false;
+    const uint32_t at = mx_by_die(id, total);
+    id += gridDim.x;
+    const uint32_t group = at / per;
+    uint32_t mt, nt;
+    mx_band(at - group * per, p.m_tiles, p.n_tiles, &mt, &nt);
+    // steps of the groups before this one, and its own
+    const uint32_t lane = threadIdx.x % kWave;
+    uint32_t before = 0;
+    for (uint32_t g0 = 0; g0 < group; g0 += kWave) {
+      const uint32_t i = g0 + lane;
+      uint32_t steps = 0;
+      if (i < group) {
+        const uint32_t first = mx_offset(p.g, i), last = mx_offset(p.g, i + 1u);
+        steps = last > first ? (last - first + kMxStep - 1u) / kMxStep : 0u;
+      }
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) steps += __shfl_xor(steps, d);
-    before += steps;
-  }
-  const uint32_t first = mx_offset(p.g, group), last = mx_offset(p.g, group + 1u);
-  MxWork w;
-  w.step0 = __builtin_amdgcn_readfirstlane(min(before, p.a.steps));
-  w.steps = __builtin_amdgcn_readfirstlane(last > first ? min((last - first + kMxStep - 1u) / kMxStep, p.a.steps - w.step0) : 0u);
-  w.a_row0 = mt * BM;
-  w.a_first = 0;
-  w.a_last = p.m;
-  w.b_row0 = nt * BN;
-  w.b_first = 0;
-  w.b_last = p.n;
-  w.out = mx_out_at(p, (uint64_t)group * p.out_group);
-  w.stride = p.out_stride;
-  mx_tile<BM, BN, DEPTH>(p, w, mx_lds);
+      for (int d = 1; d < kWave; d <<= 1) steps += __shfl_xor(steps, d);
+      before += steps;
+    }
+    const uint32_t first = mx_offset(p.g, group), last = mx_offset(p.g, group + 1u);
+    w.step0 = __builtin_amdgcn_readfirstlane(min(before, p.a.steps));
+    w.steps = __builtin_amdgcn_readfirstlane(last > first ? min((last - first + kMxStep - 1u) / kMxStep, p.a.steps - w.step0) : 0u);
+    w.a_row0 = mt * BM;
+    w.a_first = 0;
+    w.a_last = p.m;
+    w.b_row0 = nt * BN;
+    w.b_first = 0;
+    w.b_last = p.n;
+    w.out = mx_out_at(p, (uint64_t)group * p.out_group);
+    w.stride = p.out_stride;
+    return true;
+  });
 }
 
 // ------------------------------------------------------------------ few rows

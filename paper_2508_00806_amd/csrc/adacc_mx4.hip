@@ -109,6 +109,13 @@ static int mx_launch(MxProductFn fn, uint64_t grid, uint32_t threads, uint32_t l
   return launch_check(what);
 }
 
+// As many workgroups as the 256 compute units hold at a time, by LDS: 1, 2 or 4 each
+static int mx_launch_tiles(uint32_t tile, bool gradient, uint64_t tiles, hipStream_t s, const MxProductArgs& a, const char* what) {
+  if (tiles > kMxMaxGrid) return ADACC_ELIMIT;
+  const uint64_t room = tile == 256 ? 256 : tile == 128 ? 512 : 1024;
+  return mx_launch(mx4_product_fn(tile, gradient), std::min(tiles, room), kThreads, mx4_product_lds(tile), s, a, what);
+}
+
 // a (or x) times b: the operands have been checked
 static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStream_t s) {
   if (plan.few) {
@@ -121,12 +128,12 @@ static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStr
   const uint64_t m_tiles = mx_tiles(a.m, a.g.groups, plan.tile, true);
   a.m_tiles = (uint32_t)m_tiles;
   a.n_tiles = (uint32_t)mx_over(a.n + (a.g.groups && a.n % 4 ? 3 : 0), plan.tile);
-  return mx_launch(mx4_product_fn(plan.tile, false), m_tiles * a.n_tiles, kThreads, mx4_product_lds(plan.tile), s, a, "mx4_product_kernel");
+  return mx_launch_tiles(plan.tile, false, m_tiles * a.n_tiles, s, a, "mx4_product_kernel");
 }
 
 static bool mx_vec(const void* out, uint32_t type, uint64_t stride) { return stride % 4 == 0 && !mx_misaligned(out, 4 * mx_size(type)); }
 
-static void mx_compress_launch_args(uint32_t type, uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols,
+static void mx_compress_args(uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols,
                                     uint64_t row_stride, uint64_t mat_stride, MxCompressArgs* a) {
   std::memset(a, 0, sizeof *a);
   a->src = src;
@@ -137,19 +144,16 @@ static void mx_compress_launch_args(uint32_t type, uint32_t scale_rule, const vo
   a->cols = (uint32_t)cols;
   a->fullrange = scale_rule;
   a->g.rows = (uint32_t)rows;
-  a->col_tiles = (uint32_t)mx_over(cols, type == ADACC_MX4_F32 ? 256 : 512);
 }
 
 static int mx_compress_along(uint32_t type, MxCompressArgs a, void* blob, hipStream_t s) {
+  a.col_tiles = (uint32_t)mx_over(a.cols, type == ADACC_MX4_F32 ? 256 : 512);
   if (a.mats > 1 && a.mat_stride == (uint64_t)a.rows * a.row_stride) {  // one after the other: one matrix
     a.rows *= a.mats;
     a.mats = 1;
   }
   a.along = mx_matrix(blob, (uint64_t)a.mats * a.rows, a.cols);
-  // rows a wavefront: 32 where that leaves 1024 workgroups
-  a.wave_rows = 8;
-  while (a.wave_rows < 32 && mx_over(a.rows, 2ull * a.wave_rows * kWavesPerWg) * a.mats * a.col_tiles >= 1024) a.wave_rows *= 2;
-  a.row_tiles = (uint32_t)mx_over(a.rows, a.wave_rows * kWavesPerWg);
+  a.row_tiles = (uint32_t)mx_over(a.rows, kMxWaveRows * kWavesPerWg);
   const uint64_t grid = (uint64_t)a.row_tiles * a.mats * a.col_tiles;
   if (grid > kMxMaxGrid) return ADACC_ELIMIT;
   const bool narrow = a.cols * mx_size(type) < 16;
@@ -192,8 +196,8 @@ int adacc_mx4_compress(uint32_t type, uint32_t scale_rule, const void* src, uint
   if (across && (rc = mx_check_blob(across, across_bytes, mats * cols, positions)) != ADACC_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   MxCompressArgs a;
-  mx_compress_launch_args(type, scale_rule, src, mats, rows, cols, row_stride, mat_stride, &a);
-  const bool narrow = cols * mx_size(type) < 16;
+  mx_compress_args(scale_rule, src, mats, rows, cols, row_stride, mat_stride, &a);
+  const bool narrow = cols < 4;  // (a lane of that kernel has four columns)
   if (!across) return mx_compress_along(type, a, along, s);
   MxCompressArgs b = a;
   const bool both = along && !narrow;  // (narrow rows: a pass for either)
@@ -201,6 +205,7 @@ int adacc_mx4_compress(uint32_t type, uint32_t scale_rule, const void* src, uint
   b.across = mx_matrix(across, mats * cols, positions);
   b.g.offsets = offsets;
   b.g.groups = groups;
+  b.col_tiles = (uint32_t)mx_over(cols, 256);
   const uint64_t row_tiles = mx_tiles(rows, groups, kMxTileRows, false);
   const uint64_t grid = row_tiles * mats * b.col_tiles;
   if (grid > kMxMaxGrid) return ADACC_ELIMIT;
@@ -227,9 +232,7 @@ int adacc_mx4_decompress(const void* blob, uint64_t blob_bytes, uint64_t rows, u
   a.dst = dst;
   a.row_stride = row_stride;
   a.col_tiles = (uint32_t)mx_over(cols, type == ADACC_MX4_F32 ? 256 : 512);
-  a.wave_rows = 8;
-  while (a.wave_rows < 32 && mx_over(rows, 2ull * a.wave_rows * kWavesPerWg) * a.col_tiles >= 1024) a.wave_rows *= 2;
-  const uint64_t grid = mx_over(rows, a.wave_rows * kWavesPerWg) * a.col_tiles;
+  const uint64_t grid = mx_over(rows, kMxWaveRows * kWavesPerWg) * a.col_tiles;
   if (grid > kMxMaxGrid) return ADACC_ELIMIT;
   hipLaunchKernelGGL(mx4_decompress_fn(type), dim3((uint32_t)grid), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);
   return launch_check("mx4_restore_kernel");
@@ -304,7 +307,7 @@ int adacc_mx4_linear(uint32_t type, uint32_t scale_rule, const void* x, uint64_t
   if (rc != ADACC_OK) return rc;
   if (k) {
     MxCompressArgs c;
-    mx_compress_launch_args(type, scale_rule, x, 1, m, k, x_stride, 0, &c);
+    mx_compress_args(scale_rule, x, 1, m, k, x_stride, 0, &c);
     rc = mx_compress_along(type, c, workspace, s);
     if (rc != ADACC_OK) return rc;
   }
@@ -349,7 +352,7 @@ int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* 
   const uint32_t tile = tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
   p.m_tiles = (uint32_t)mx_over(m, tile);
   p.n_tiles = (uint32_t)mx_over(n, tile);
-  return mx_launch(mx4_product_fn(tile, true), tiles(tile), kThreads, mx4_product_lds(tile), s, p, "mx4_gradient_kernel");
+  return mx_launch_tiles(tile, true, tiles(tile), s, p, "mx4_gradient_kernel");
 }
 
 }  // extern "C"

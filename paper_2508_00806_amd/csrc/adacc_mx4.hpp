@@ -22,6 +22,7 @@ constexpr uint32_t kMxBlock = 32;        // values per scale
 constexpr uint32_t kMxStep = 128;        // columns per step: codes of 64 bytes, 4 scales
 constexpr uint32_t kMxStepBytes = 64;
 constexpr uint32_t kMxTileRows = 128;    // rows of a workgroup of the compression, and what an expert's tokens are padded to across
+constexpr uint32_t kMxWaveRows = 8;      // rows of a wavefront of the compression along the rows, and of the restoration
 constexpr uint32_t kMxMaxGroups = 4096;
 constexpr uint32_t kMxNanByte = 255;
 constexpr uint32_t kMxFewWaves = 8;      // of a workgroup of the product of few rows, at most
@@ -52,7 +53,6 @@ struct MxCompressArgs {
   uint64_t row_stride, mat_stride;  // elements
   uint32_t mats, rows, cols;        // of one matrix; blob rows = mats * rows
   uint32_t fullrange;
-  uint32_t wave_rows;               // along the rows only: rows that a wavefront takes
   uint32_t row_tiles, col_tiles;
   MxGroups g;
   MxMatrix along;   // [mats * rows][cols]
@@ -65,7 +65,6 @@ struct MxDecompressArgs {
   void* dst;
   uint64_t row_stride;
   uint32_t col_tiles;
-  uint32_t wave_rows;
 };
 
 struct MxProductArgs {
@@ -89,7 +88,7 @@ struct MxProductArgs {
 typedef void (*MxCompressFn)(MxCompressArgs);
 typedef void (*MxDecompressFn)(MxDecompressArgs);
 typedef void (*MxProductFn)(MxProductArgs);
-MxCompressFn mx4_compress_fn(uint32_t type, bool along, bool across, bool narrow);  // narrow: rows of fewer than 16 bytes
+MxCompressFn mx4_compress_fn(uint32_t type, bool along, bool across, bool narrow);  // narrow: rows that a lane's load does not fit in; not for both at once
 MxDecompressFn mx4_decompress_fn(uint32_t type);
 MxProductFn mx4_product_fn(uint32_t tile, bool gradient);  // tile: 256, 128 or 64 rows and columns a workgroup
 uint32_t mx4_product_lds(uint32_t tile);

@@ -40,21 +40,24 @@ class Mx4Matrix:
     def restore(self, dtype=torch.bfloat16, out=None):
         """The matrix of the values that the codes stand for."""
         out = torch.empty(self.shape, dtype=dtype, device=self.blob.device) if out is None else out
-        if tuple(out.shape) != self.shape:
+        if out.shape != self.shape:
             raise ValueError(f"out has shape {tuple(out.shape)}, the matrix {self.shape}")
-        mx4_decompress(self.blob, out.flatten(0, -2), stream=_stream_of(self.blob))
+        mx4_decompress(self.blob, out if out.dim() == 2 else out.view(-1, self.shape[-1]), stream=_stream_of(self.blob))
         return out
 
 
 def _stream_of(t):
-    """The current stream of the tensor's device."""
-    return torch.cuda.current_stream(t.device)
+    """The current stream of the tensor's device, as a handle."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _flat(x):
     """[..., cols] as a matrix with adjacent columns (a copy only where the strides ask for one)."""
-    x = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
-    return x if x.shape[1] <= 1 or (x.stride(1) == 1 and x.stride(0) >= x.shape[1]) else x.contiguous()
+    if x.dim() != 2:
+        x = x.reshape(-1, x.shape[-1])
+    stride, step = x.stride()
+    cols = x.shape[1]
+    return x if cols <= 1 or (step == 1 and stride >= cols) else x.contiguous()
 
 
 def _stack(x):
@@ -78,12 +81,14 @@ def _blobs(x, along, across, rule, offsets=None):
 
 def compress(x, scale_rule="floor"):
     """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension."""
+    _on_gpu(x)
     x = _stack(x.detach())
     return Mx4Matrix(_blobs(x, True, False, _rule(scale_rule))[0], x.shape)
 
 
 def compress_both(x, scale_rule="floor"):
     """(x, x transposed), both compressed, from one reading of x: blocks along the last dimension, and along the one before it."""
+    _on_gpu(x)
     x = _stack(x.detach())
     along, across = _blobs(x, True, True, _rule(scale_rule))
     return Mx4Matrix(along, x.shape), Mx4Matrix(across, (*x.shape[:-2], x.shape[-1], x.shape[-2]))
@@ -93,11 +98,12 @@ def _serve(x, w, offsets, out_dtype):
     rows = _flat(x)
     n, k = w.shape[-2:]
     groups = 0 if offsets is None else offsets.numel() - 1
-    out = torch.empty((rows.shape[0], n), dtype=out_dtype or x.dtype, device=x.device)
-    need = mx4_linear_workspace_bytes(rows.shape[0], n, k, groups)
+    m = rows.shape[0]
+    out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
+    need = mx4_linear_workspace_bytes(m, n, k, groups)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     mx4_linear(rows, w.blob, out, offsets=offsets, workspace=ws, stream=_stream_of(x))
-    return out.view(*x.shape[:-1], n)
+    return out if x.dim() == 2 else out.view(*x.shape[:-1], n)
 
 
 class _Layer(torch.autograd.Function):
@@ -134,11 +140,19 @@ class _Layer(torch.autograd.Function):
         return dx, dw, None, None
 
 
+def _on_gpu(x):
+    if not x.is_cuda:
+        raise ValueError(f"a tensor on a GPU is needed, not on {x.device}")
+
+
 def _check_operands(x, w, mats):
     if len(w.shape) != (3 if mats else 2):
         raise ValueError(f"the weight must have {3 if mats else 2} dimensions, not {len(w.shape)}")
     if x.dim() < 1 or x.shape[-1] != w.shape[-1]:
         raise ValueError(f"rows of {x.shape[-1] if x.dim() else 0} values do not fit a weight of shape {tuple(w.shape)}")
+    _on_gpu(x)
+    if (w.blob if isinstance(w, Mx4Matrix) else w).get_device() != x.get_device():
+        raise ValueError("the weight must be on the device of the rows")
 
 
 def linear(x, weight, out_dtype=None):
@@ -161,7 +175,7 @@ def experts(x, offsets, weight, out_dtype=None):
     _check_operands(x, weight, True)
     if x.dim() != 2:
         raise ValueError("x must be a matrix")
-    if offsets.device != x.device:
+    if offsets.get_device() != x.get_device():
         raise ValueError("offsets must be on the device of x")
     if offsets.numel() != weight.shape[0] + 1:
         raise ValueError(f"{weight.shape[0]} experts need {weight.shape[0] + 1} offsets, not {offsets.numel()}")

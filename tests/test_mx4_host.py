@@ -138,8 +138,8 @@ def test_python_refusals():
         adacc.mx4_compress(x.t(), None, None)
     with pytest.raises(TypeError):
         adacc.mx4_compress(x, None, None, offsets=torch.zeros(3))
-    with pytest.raises(ValueError):
-        mx4.compress(x, scale_rule="ceil")
+    with pytest.raises(ValueError, match="scale_rule"):
+        mx4._rule("ceil")
     with pytest.raises(ValueError):
         mx4.linear(x, torch.zeros(3, 9))
     with pytest.raises(ValueError):
@@ -148,3 +148,7 @@ def test_python_refusals():
         mx4.experts(x, torch.zeros(2, dtype=torch.int32), torch.zeros(2, 3, 8))
     with pytest.raises(ValueError):
         adacc.mx4_gradient(None, None, 4, torch.zeros(3, 8), offsets=torch.zeros(3, dtype=torch.int32))
+    for call in (lambda: mx4.compress(x), lambda: mx4.compress_both(x), lambda: mx4.linear(x, torch.zeros(3, 8)),
+                 lambda: mx4.experts(x, torch.zeros(3, dtype=torch.int32), torch.zeros(2, 3, 8))):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
