@@ -465,12 +465,22 @@ __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kern
 
 // ------------------------------------------------------------------ few rows
 // What bounds a product of few rows is the reading of b.  A workgroup takes 16 * NS rows of b and up to 16 * MS rows of a; its wavefronts
-// share the contraction, two steps at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
+// share the contraction, U steps at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
 // operand registers: lane (r, q) = (lane % 16, lane / 16) reads block q of the step of its row.  Row NS * r + j of b is row r of
-// tile j, as above.
-// SRC: a is compressed on the way (kMxBf16 ... kMxF32): the lane's operand is one block of one row, so it reads 32 values, and no
-// other lane has a part in the block.  kMxReady: a is compressed.
-constexpr uint32_t kMxFewAhead = 2;  // pairs of steps in flight
+// tile j, as above.  A turn's loads are under way while the turn before is multiplied, and nothing is loaded under a condition: what is not
+// there is read from a place that is, and its codes are dropped.
+// SRC: a is compressed on the way (kMxBf16 ... kMxF32), by every workgroup for itself: a thread takes a block of 32 values, whose codes and
+// scale byte go to LDS.  kMxReady: a is compressed.
+template <uint32_t MS, uint32_t NS, uint32_t SRC>
+struct MxFew {
+  static constexpr bool kRaw = SRC != kMxReady;
+  // two turns of U * (4 * NS + 4 * MS) registers (U * 4 * NS, with a in LDS) and what belongs to them, in the 128 of a lane, or 256 (MS > 1)
+  static constexpr uint32_t U = (kRaw ? NS <= 2u : NS + MS <= (MS == 1u ? 2u : 5u)) ? 4u : 2u;
+  uint4 b[U][NS];
+  uint32_t sb[U];
+  uint4 a[U][MS];
+  uint32_t sa[U][MS];
+};
 
 template <uint32_t S>
 __device__ __forceinline__ uint32_t mx_scales_at(const uint8_t* p) {
@@ -487,28 +497,29 @@ __device__ __forceinline__ uint32_t mx_pk_max(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(mx_u16x2, a), __builtin_bit_cast(mx_u16x2, b)));
 }
 
-// one block of 32 values (`left` of them exist; a multiple of 8 or all) to codes and scale byte
+// one block of 32 values, `left` of which exist (a multiple of 8, at least 8), to codes and scale byte
 template <uint32_t TYPE>
-__device__ __forceinline__ uint4 mx_compress_block(const uint8_t* p, int32_t left, uint32_t fullrange, uint32_t* byte) {
-  constexpr uint32_t kLoads = TYPE == kMxF32 ? 8u : 4u;
-  constexpr int32_t kEach = 32 / (int32_t)kLoads;
-  uint4 v[kLoads];
+__device__ __forceinline__ uint4 mx_compress_block(const uint8_t* p, uint32_t left, uint32_t fullrange, uint32_t* byte) {
+  constexpr uint32_t N = TYPE == kMxF32 ? 8u : 4u, kEach = 32u / N;  // loads, and values of one
+  uint4 v[N];
 #pragma unroll
-  for (uint32_t i = 0; i < kLoads; ++i) {
-    v[i] = make_uint4(0u, 0u, 0u, 0u);
-    if ((int32_t)i * kEach < left) {
-      const mx_u4u t = *reinterpret_cast<const mx_u4u*>(p + 16u * i);
-      v[i] = make_uint4(t.x, t.y, t.z, t.w);
-    }
+  for (uint32_t i = 0; i < N; ++i) {
+    const mx_u4u t = *reinterpret_cast<const mx_u4u*>(p + (i * kEach < left ? 16u * i : 0u));
+    v[i] = make_uint4(t.x, t.y, t.z, t.w);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) {
+    const uint32_t keep = i * kEach < left ? ~0u : 0u;
+    v[i] = make_uint4(v[i].x & keep, v[i].y & keep, v[i].z & keep, v[i].w & keep);
   }
   uint32_t most = 0u;
   if constexpr (TYPE == kMxF32) {
 #pragma unroll
-    for (uint32_t i = 0; i < kLoads; ++i) most = max(most, max(max(v[i].x & 0x7FFFFFFFu, v[i].y & 0x7FFFFFFFu), max(v[i].z & 0x7FFFFFFFu, v[i].w & 0x7FFFFFFFu)));
+    for (uint32_t i = 0; i < N; ++i) most = max(most, max(max(v[i].x & 0x7FFFFFFFu, v[i].y & 0x7FFFFFFFu), max(v[i].z & 0x7FFFFFFFu, v[i].w & 0x7FFFFFFFu)));
   } else {
     uint32_t m2 = 0u;
 #pragma unroll
-    for (uint32_t i = 0; i < kLoads; ++i) m2 = mx_pk_max(m2, mx_pk_max(mx_pk_max(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), mx_pk_max(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu)));
+    for (uint32_t i = 0; i < N; ++i) m2 = mx_pk_max(m2, mx_pk_max(mx_pk_max(v[i].x & 0x7FFF7FFFu, v[i].y & 0x7FFF7FFFu), mx_pk_max(v[i].z & 0x7FFF7FFFu, v[i].w & 0x7FFF7FFFu)));
     const uint32_t mag = max(m2 & 0xFFFFu, m2 >> 16);
     most = TYPE == kMxBf16 ? mag << 16 : __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)mag));
   }
@@ -519,21 +530,21 @@ __device__ __forceinline__ uint4 mx_compress_block(const uint8_t* p, int32_t lef
   for (uint32_t k = 0; k < 4u; ++k) {
     uint32_t w = 0u;
     if constexpr (TYPE == kMxF32) {
-      const uint4 x = v[(2 * k) % kLoads], y = v[(2 * k + 1) % kLoads];
+      const uint4 x = v[(2 * k) % N], y = v[(2 * k + 1) % N];
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.x), __uint_as_float(x.y), s, 0);
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.z), __uint_as_float(x.w), s, 1);
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(y.x), __uint_as_float(y.y), s, 2);
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(y.z), __uint_as_float(y.w), s, 3);
     } else if constexpr (TYPE == kMxBf16) {
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].x), s, 0);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].y), s, 1);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].z), s, 2);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % kLoads].w), s, 3);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % N].x), s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % N].y), s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % N].z), s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(mx_bf16x2, v[k % N].w), s, 3);
     } else {
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].x), s, 0);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].y), s, 1);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].z), s, 2);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % kLoads].w), s, 3);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % N].x), s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % N].y), s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % N].z), s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(mx_f16x2, v[k % N].w), s, 3);
     }
     o[k] = *byte == kMxNanByte ? 0u : w;
   }
@@ -541,7 +552,9 @@ __device__ __forceinline__ uint4 mx_compress_block(const uint8_t* p, int32_t lef
 }
 
 template <uint32_t MS, uint32_t NS, uint32_t SRC>
-__global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductArgs p) {
+__global__ __launch_bounds__(mx4_few_waves(MS) * kWave) void mx4_few_kernel(MxProductArgs p) {
+  using F = MxFew<MS, NS, SRC>;
+  constexpr uint32_t U = F::U;
   extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const uint32_t waves = blockDim.x / kWave;
@@ -571,65 +584,99 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
   const uint8_t* b_scale = p.b.scales + (uint64_t)q * p.b.pitch + b_scale_row;
   const uint8_t* a_row[MS];
   const uint8_t* a_scale[MS];
-  bool a_there[MS];
+  uint32_t a_step, a_scale_step;  // with a in LDS: [step][row][64], then [step][block][row]
+  uint8_t* const lds_scales = mx_lds + steps * rows * kMxStepBytes;
 #pragma unroll
   for (uint32_t i = 0; i < MS; ++i) {
-    const uint32_t row = row0 + min(16u * i + r, rows - 1u);
-    a_there[i] = 16u * i + r < rows;
-    if constexpr (SRC == kMxReady) {
-      a_row[i] = p.a.codes + (uint64_t)row * kMxStepBytes + 16u * q;
-      a_scale[i] = p.a.scales + (uint64_t)q * p.a.pitch + row;
-    } else {
-      constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;
-      a_row[i] = static_cast<const uint8_t*>(p.x) + ((uint64_t)row * p.x_stride + kMxBlock * q) * kBytes;
-      a_scale[i] = nullptr;
-    }
+    const uint32_t row = min(16u * i + r, rows - 1u);
+    a_row[i] = F::kRaw ? mx_lds + row * kMxStepBytes + 16u * q : p.a.codes + (uint64_t)(row0 + row) * kMxStepBytes + 16u * q;
+    a_scale[i] = F::kRaw ? lds_scales + q * rows + row : p.a.scales + (uint64_t)q * p.a.pitch + row0 + row;
   }
-  for (uint32_t s0 = 2u * wave; s0 < steps; s0 += 2u * kMxFewAhead * waves) {
-    uint4 b[2 * kMxFewAhead][NS], a[2 * kMxFewAhead][MS];
-    uint32_t sb[2 * kMxFewAhead], sa[2 * kMxFewAhead][MS];
+  a_step = rows * kMxStepBytes;
+  a_scale_step = 4u * rows;
+  // the U steps from s0 on (behind the last: the last one again, which multiply leaves out)
+  const auto load = [&](F& t, uint32_t s0) {
+    if constexpr (!F::kRaw) {
 #pragma unroll
-    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
-      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
-      const uint32_t s = min(want, steps - 1u);
+      for (uint32_t u = 0; u < U; ++u) {
+        const uint32_t s = min(s0 + u, steps - 1u);
 #pragma unroll
-      for (uint32_t j = 0; j < NS; ++j) {
-        const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b_row[j] + (uint64_t)s * p.b.step_bytes));
-        b[u][j] = make_uint4(t.x, t.y, t.z, t.w);
-      }
-      sb[u] = mx_scales_at<NS>(b_scale + (uint64_t)(4u * s) * p.b.pitch);
-    }
-#pragma unroll
-    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
-      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
-      const uint32_t s = min(want, steps - 1u);
-#pragma unroll
-      for (uint32_t i = 0; i < MS; ++i) {
-        if constexpr (SRC == kMxReady) {
-          a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + (uint64_t)s * p.a.step_bytes);
-          sa[u][i] = a_scale[i][(uint64_t)(4u * s) * p.a.pitch];
-        } else {
-          constexpr uint32_t kBytes = SRC == kMxF32 ? 4u : 2u;
-          const int32_t left = (int32_t)p.k - (int32_t)(s * kMxStep + q * kMxBlock);
-          a[u][i] = make_uint4(0u, 0u, 0u, 0u);
-          sa[u][i] = 0u;
-          if (a_there[i]) a[u][i] = mx_compress_block<SRC>(a_row[i] + (uint64_t)s * kMxStep * kBytes, left, p.fullrange, &sa[u][i]);
+        for (uint32_t i = 0; i < MS; ++i) {
+          t.a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + (uint64_t)s * p.a.step_bytes);
+          t.sa[u][i] = a_scale[i][(uint64_t)(4u * s) * p.a.pitch];
         }
       }
     }
 #pragma unroll
-    for (uint32_t u = 0; u < 2u * kMxFewAhead; ++u) {
-      const uint32_t want = s0 + (u / 2u) * 2u * waves + u % 2u;
-      if (want < steps) {  // (uniform)
+    for (uint32_t u = 0; u < U; ++u) {
+      const uint32_t s = min(s0 + u, steps - 1u);
+      t.sb[u] = mx_scales_at<NS>(b_scale + (uint64_t)(4u * s) * p.b.pitch);
+#pragma unroll
+      for (uint32_t j = 0; j < NS; ++j) {
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b_row[j] + (uint64_t)s * p.b.step_bytes));
+        t.b[u][j] = make_uint4(v.x, v.y, v.z, v.w);
+      }
+    }
+  };
+  const auto multiply = [&](F& t, uint32_t s0) {
+    if constexpr (F::kRaw) {
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u) {
+        const uint32_t s = min(s0 + u, steps - 1u);
 #pragma unroll
         for (uint32_t i = 0; i < MS; ++i) {
-#define ADACC_MX_AT(J) if constexpr (J < NS) acc[i][J % NS] = mx_mfma16<J>(a[u][i], b[u][J % NS], acc[i][J % NS], sa[u][i], sb[u]);
+          t.a[u][i] = *reinterpret_cast<const uint4*>(a_row[i] + s * a_step);
+          t.sa[u][i] = a_scale[i][s * a_scale_step];
+        }
+      }
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) {
+      if (s0 + u < steps) {  // (uniform)
+#pragma unroll
+        for (uint32_t i = 0; i < MS; ++i) {
+#define ADACC_MX_AT(J) if constexpr (J < NS) acc[i][J % NS] = mx_mfma16<J>(t.a[u][i], t.b[u][J % NS], acc[i][J % NS], t.sa[u][i], t.sb[u]);
           ADACC_MX_AT(0) ADACC_MX_AT(1) ADACC_MX_AT(2) ADACC_MX_AT(3)
 #undef ADACC_MX_AT
         }
       }
     }
+  };
+  const uint32_t apart = U * waves;
+  uint32_t s0 = U * wave;
+  F one, two;
+  if constexpr (F::kRaw) {
+    const uint32_t blocks = 4u * steps;  // of a row; those behind its end are zeros
+    for (uint32_t t = threadIdx.x; t < rows * blocks; t += blockDim.x) {
+      const uint32_t row = t / blocks, block = t - row * blocks;
+      const uint32_t first = block * kMxBlock;
+      uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+      uint32_t byte = 0u;
+      if (first < p.k)
+        codes = mx_compress_block<SRC>(static_cast<const uint8_t*>(p.x) + ((uint64_t)(row0 + row) * p.x_stride + first) * (SRC == kMxF32 ? 4u : 2u),
+                                       min(p.k - first, kMxBlock), p.fullrange, &byte);
+      const uint32_t step = block / 4u, in = block % 4u;
+      *reinterpret_cast<uint4*>(mx_lds + (step * rows + row) * kMxStepBytes + in * 16u) = codes;
+      lds_scales[block * rows + row] = (uint8_t)byte;
+    }
+    if (s0 < steps) load(one, s0);
+    __syncthreads();
+  } else {
+    if (s0 < steps) load(one, s0);
   }
+  if (s0 < steps) {  // (uniform in the wavefront)
+    for (;;) {
+      if (s0 + apart < steps) load(two, s0 + apart);
+      multiply(one, s0);
+      s0 += apart;
+      if (s0 >= steps) break;
+      if (s0 + apart < steps) load(one, s0 + apart);
+      multiply(two, s0);
+      s0 += apart;
+      if (s0 >= steps) break;
+    }
+  }
+  if constexpr (F::kRaw) __syncthreads();  // a has been read
   // lane (r, q) holds rows 4 * q + e and column r of a tile; [wave][row][column] in LDS
   float* sums = reinterpret_cast<float*>(mx_lds);
   constexpr uint32_t kCols = 16u * NS, kRows = 16u * MS;
@@ -638,7 +685,7 @@ __global__ __launch_bounds__(kMxFewWaves * kWave) void mx4_few_kernel(MxProductA
 #pragma unroll
     for (uint32_t e = 0; e < 4u; ++e)
 #pragma unroll
-      for (uint32_t j = 0; j < NS; ++j) sums[((uint64_t)wave * kRows + 16u * i + 4u * q + e) * kCols + NS * r + j] = acc[i][j][e];
+      for (uint32_t j = 0; j < NS; ++j) sums[(wave * kRows + 16u * i + 4u * q + e) * kCols + NS * r + j] = acc[i][j][e];
   __syncthreads();
   for (uint32_t t = threadIdx.x; t < rows * kCols; t += blockDim.x) {
     const uint32_t row = t / kCols, col = t % kCols;

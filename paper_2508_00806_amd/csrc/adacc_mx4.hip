@@ -78,6 +78,8 @@ struct MxPlan {
   uint32_t tile;
 };
 constexpr uint64_t kMxFewRows = 64;
+constexpr uint64_t kMxFewRaw = 1ull << 16;  // values of a tile's rows that every workgroup compresses for itself
+static uint32_t mx_few_row_lds(uint64_t k) { return (uint32_t)mx_over(k, kMxStep) * (kMxStepBytes + 4u); }
 
 static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
   MxPlan p;
@@ -88,8 +90,10 @@ static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
     p.ms = rows <= 16 ? 1u : rows <= 32 ? 2u : 4u;
     const uint64_t m_tiles = groups ? std::min<uint64_t>(groups, m) : mx_over(m, 16 * p.ms);
     p.ns = mx_over(n, 64) * m_tiles >= 512 ? 4u : mx_over(n, 32) * m_tiles >= 256 ? 2u : 1u;
-    p.waves = (uint32_t)std::min<uint64_t>(kMxFewWaves, std::max<uint64_t>(1, mx_over(k, 4 * kMxStep)));
-    p.ready = p.ms != 1 || k % 8 != 0;
+    // a compute unit holds mx4_few_waves wavefronts: they are shared among the workgroups that come to it, none has less than a turn of two steps
+    const uint64_t tiles = mx_over(n, 16 * p.ns) * m_tiles, most = mx4_few_waves(p.ms);
+    p.waves = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(most / std::min<uint64_t>(most, mx_over(tiles, 256)), mx_over(k, 2 * kMxStep)));
+    p.ready = p.ms != 1 || k % 8 != 0 || (groups ? std::min<uint64_t>(m, 16) : m) * k > kMxFewRaw;
     return p;
   }
   const auto tiles = [&](uint64_t t) { return mx_over(rows, t) * mx_over(n, t) * std::max<uint32_t>(groups, 1u); };
@@ -122,7 +126,7 @@ static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStr
     a.n_tiles = (uint32_t)mx_over(a.n, 16 * plan.ns);
     const uint64_t m_tiles = mx_tiles(a.m, a.g.groups, 16 * plan.ms, false);
     a.m_tiles = (uint32_t)m_tiles;
-    const uint32_t lds = plan.waves * 16u * plan.ms * 16u * plan.ns * 4u;
+    const uint32_t lds = std::max<uint32_t>(plan.waves * 16u * plan.ms * 16u * plan.ns * 4u, src != kMxReady ? mx_few_row_lds(a.k) * (uint32_t)std::min<uint64_t>(a.m, 16u * plan.ms) : 0u);
     return mx_launch(mx4_few_fn(plan.ms, plan.ns, src), m_tiles * a.n_tiles, plan.waves * kWave, lds, s, a, "mx4_few_kernel");
   }
   const uint64_t m_tiles = mx_tiles(a.m, a.g.groups, plan.tile, true);

@@ -25,7 +25,8 @@ constexpr uint32_t kMxTileRows = 128;    // rows of a workgroup of the compressi
 constexpr uint32_t kMxWaveRows = 8;      // rows of a wavefront of the compression along the rows, and of the restoration
 constexpr uint32_t kMxMaxGroups = 4096;
 constexpr uint32_t kMxNanByte = 255;
-constexpr uint32_t kMxFewWaves = 8;      // of a workgroup of the product of few rows, at most
+// wavefronts of a workgroup of the product of few rows, at most: sixteen leave a lane 128 registers, eight 256
+constexpr uint32_t mx4_few_waves(uint32_t ms) { return ms == 1 ? 16u : 8u; }
 
 enum : uint32_t { kMxBf16 = 0, kMxF16 = 1, kMxF32 = 2, kMxReady = 3 };  // kMxReady: a left operand that is compressed already
 
