@@ -635,6 +635,24 @@ def mask_unpack(bits, mask, n=None, stream=None):
 # ---------------------------------------------------------------- microscaled 4-bit matrices and their products
 MX4_BF16, MX4_F16, MX4_F32 = 0, 1, 2
 MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE = 0, 1
+_MX4_CALLS = ("mx4_compress", "mx4_decompress", "mx4_product", "mx4_linear", "mx4_gradient", "mx4_linear_workspace_bytes")
+_mx4_entries = {}
+
+
+def _mx4(name):
+    """The library's function adacc_<name>: marshalled natively, or by ctypes where that is not to be had (2 us a call more)."""
+    entry = _mx4_entries.get(name)
+    if entry is None:
+        L = lib()
+        general = {n: getattr(L, "adacc_" + n) for n in _MX4_CALLS}
+        native = calls()
+        try:
+            native.bind_mx4(*[ctypes.cast(f, ctypes.c_void_p).value for f in general.values()])
+            _mx4_entries.update({n: getattr(native, n) for n in _MX4_CALLS})
+        except TypeError:
+            _mx4_entries.update(general)
+        entry = _mx4_entries[name]
+    return entry
 
 
 def mx4_layout_of(rows: int, cols: int) -> CMx4Layout:
@@ -699,7 +717,7 @@ def mx4_compress(src, along=None, across=None, offsets=None, scale_rule=MX4_SCAL
     row_stride = src.stride(-2) if rows > 1 else cols
     mat_stride = src.stride(0) if src.dim() == 3 and mats > 1 else 0
     off, groups = _mx4_groups(offsets)
-    _check(lib().adacc_mx4_compress(kind, scale_rule, _ptr(src), mats, rows, cols, row_stride, mat_stride, off, groups, *_mx4_blob(along),
+    _check(_mx4("mx4_compress")(kind, scale_rule, _ptr(src), mats, rows, cols, row_stride, mat_stride, off, groups, *_mx4_blob(along),
                                     *_mx4_blob(across), _stream(stream)), "adacc_mx4_compress")
 
 
@@ -707,7 +725,7 @@ def mx4_decompress(blob, dst, stream=None):
     """dst: a matrix with adjacent columns, of the blob's shape."""
     kind = _mx4_type(dst)
     stride = _mx4_rows(dst, "dst")
-    _check(lib().adacc_mx4_decompress(*_mx4_blob(blob), dst.shape[0], dst.shape[1], _ptr(dst), kind, stride, _stream(stream)),
+    _check(_mx4("mx4_decompress")(*_mx4_blob(blob), dst.shape[0], dst.shape[1], _ptr(dst), kind, stride, _stream(stream)),
            "adacc_mx4_decompress")
 
 
@@ -717,12 +735,12 @@ def mx4_product(a, b, k: int, out, offsets=None, stream=None):
     stride = _mx4_rows(out, "out")
     off, groups = _mx4_groups(offsets)
     m, n = out.shape
-    _check(lib().adacc_mx4_product(*_mx4_blob(a), m, *_mx4_blob(b), n, k, off, groups, _ptr(out), kind, stride, _stream(stream)),
+    _check(_mx4("mx4_product")(*_mx4_blob(a), m, *_mx4_blob(b), n, k, off, groups, _ptr(out), kind, stride, _stream(stream)),
            "adacc_mx4_product")
 
 
 def mx4_linear_workspace_bytes(m: int, n: int, k: int, groups: int = 0) -> int:
-    return int(lib().adacc_mx4_linear_workspace_bytes(m, n, k, groups))
+    return int(_mx4("mx4_linear_workspace_bytes")(m, n, k, groups))
 
 
 def mx4_linear(x, b, out, offsets=None, workspace=None, scale_rule=MX4_SCALE_FLOOR, stream=None):
@@ -735,7 +753,7 @@ def mx4_linear(x, b, out, offsets=None, workspace=None, scale_rule=MX4_SCALE_FLO
     n = out.shape[1]
     if out.shape[0] != m:
         raise ValueError(f"out has {out.shape[0]} rows, x has {m}")
-    _check(lib().adacc_mx4_linear(kind, scale_rule, _ptr(x), m, x_stride, *_mx4_blob(b), n, k, off, groups, _ptr(out), okind, o_stride,
+    _check(_mx4("mx4_linear")(kind, scale_rule, _ptr(x), m, x_stride, *_mx4_blob(b), n, k, off, groups, _ptr(out), okind, o_stride,
                                   *_mx4_blob(workspace), _stream(stream)), "adacc_mx4_linear")
 
 
@@ -747,7 +765,7 @@ def mx4_gradient(a, b, rows: int, out, offsets=None, stream=None):
     if out.dim() != (3 if groups else 2) or not out.is_contiguous() or (groups and out.shape[0] != groups):
         raise ValueError("out must be a contiguous [groups, m, n], or [m, n] without offsets")
     m, n = out.shape[-2:]
-    _check(lib().adacc_mx4_gradient(*_mx4_blob(a), m, *_mx4_blob(b), n, rows, off, groups, _ptr(out), kind, n, _stream(stream)),
+    _check(_mx4("mx4_gradient")(*_mx4_blob(a), m, *_mx4_blob(b), n, rows, off, groups, _ptr(out), kind, n, _stream(stream)),
            "adacc_mx4_gradient")
 
 

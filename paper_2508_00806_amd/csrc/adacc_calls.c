@@ -207,6 +207,78 @@ static PyObject *channelwise_decompress(PyObject *self, PyObject *const *a, Py_s
   CALL(channelwise_decompress_call((uint32_t)bits, (uint32_t)format, blob, bytes, tokens, (uint32_t)hidden, dst, (int)type, stream));
 }
 
+// ---- microscaled matrices: the binding has the numbers in hand already; an address may be None
+typedef int (*mx4_compress_fn)(uint32_t, uint32_t, const void *, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, const int32_t *, uint32_t, void *,
+                                uint64_t, void *, uint64_t, void *);
+typedef int (*mx4_decompress_fn)(const void *, uint64_t, uint64_t, uint64_t, void *, uint32_t, uint64_t, void *);
+typedef int (*mx4_product_fn)(const void *, uint64_t, uint64_t, const void *, uint64_t, uint64_t, uint64_t, const int32_t *, uint32_t, void *, uint32_t,
+                               uint64_t, void *);
+typedef int (*mx4_linear_fn)(uint32_t, uint32_t, const void *, uint64_t, uint64_t, const void *, uint64_t, uint64_t, uint64_t, const int32_t *, uint32_t,
+                              void *, uint32_t, uint64_t, void *, uint64_t, void *);
+typedef int (*mx4_gradient_fn)(const void *, uint64_t, uint64_t, const void *, uint64_t, uint64_t, uint64_t, const int32_t *, uint32_t, void *, uint32_t,
+                                uint64_t, void *);
+typedef uint64_t (*mx4_workspace_fn)(uint64_t, uint64_t, uint64_t, uint32_t);
+static mx4_compress_fn mx4_compress_call;
+static mx4_decompress_fn mx4_decompress_call;
+static mx4_product_fn mx4_product_call;
+static mx4_linear_fn mx4_linear_call;
+static mx4_gradient_fn mx4_gradient_call;
+static mx4_workspace_fn mx4_workspace_call;
+
+static int numbers(PyObject *const *a, Py_ssize_t n, Py_ssize_t want, uint64_t *v) {
+  if (!arguments(n, want)) return 0;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    v[i] = 0;
+    if (a[i] != Py_None && !to_u64(a[i], &v[i])) return 0;
+  }
+  return 1;
+}
+#define P(i) ((void *)(uintptr_t)v[i])
+static PyObject *mx4_compress(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[15];
+  if (!numbers(a, n, 15, v)) return NULL;
+  CALL(mx4_compress_call((uint32_t)v[0], (uint32_t)v[1], P(2), v[3], v[4], v[5], v[6], v[7], P(8), (uint32_t)v[9], P(10), v[11], P(12), v[13], P(14)));
+}
+static PyObject *mx4_decompress(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[8];
+  if (!numbers(a, n, 8, v)) return NULL;
+  CALL(mx4_decompress_call(P(0), v[1], v[2], v[3], P(4), (uint32_t)v[5], v[6], P(7)));
+}
+static PyObject *mx4_product(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[13];
+  if (!numbers(a, n, 13, v)) return NULL;
+  CALL(mx4_product_call(P(0), v[1], v[2], P(3), v[4], v[5], v[6], P(7), (uint32_t)v[8], P(9), (uint32_t)v[10], v[11], P(12)));
+}
+static PyObject *mx4_linear(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[17];
+  if (!numbers(a, n, 17, v)) return NULL;
+  CALL(mx4_linear_call((uint32_t)v[0], (uint32_t)v[1], P(2), v[3], v[4], P(5), v[6], v[7], v[8], P(9), (uint32_t)v[10], P(11), (uint32_t)v[12], v[13],
+                       P(14), v[15], P(16)));
+}
+static PyObject *mx4_gradient(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[13];
+  if (!numbers(a, n, 13, v)) return NULL;
+  CALL(mx4_gradient_call(P(0), v[1], v[2], P(3), v[4], v[5], v[6], P(7), (uint32_t)v[8], P(9), (uint32_t)v[10], v[11], P(12)));
+}
+static PyObject *mx4_linear_workspace_bytes(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[4];
+  if (!numbers(a, n, 4, v)) return NULL;
+  return PyLong_FromUnsignedLongLong(mx4_workspace_call(v[0], v[1], v[2], (uint32_t)v[3]));
+}
+// bind_mx4(addresses of the six functions, in the order above)
+static PyObject *bind_mx4(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  uint64_t v[6];
+  if (!numbers(a, n, 6, v)) return NULL;
+  mx4_compress_call = (mx4_compress_fn)(uintptr_t)v[0];
+  mx4_decompress_call = (mx4_decompress_fn)(uintptr_t)v[1];
+  mx4_product_call = (mx4_product_fn)(uintptr_t)v[2];
+  mx4_linear_call = (mx4_linear_fn)(uintptr_t)v[3];
+  mx4_gradient_call = (mx4_gradient_fn)(uintptr_t)v[4];
+  mx4_workspace_call = (mx4_workspace_fn)(uintptr_t)v[5];
+  Py_RETURN_NONE;
+}
+#undef P
+
 // bind(addresses of the eight functions, float32, bfloat16, float16, is_initialized, current device, raw stream, general stream)
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   uint64_t f[8];
@@ -231,7 +303,9 @@ static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef functions[] = {ENTRY(bind), ENTRY(compress), ENTRY(decompress), ENTRY(mask_pack), ENTRY(mask_unpack), ENTRY(channel_compress),
-                                  ENTRY(channel_decompress), ENTRY(channelwise_compress), ENTRY(channelwise_decompress), {NULL, NULL, 0, NULL}};
+                                  ENTRY(channel_decompress), ENTRY(channelwise_compress), ENTRY(channelwise_decompress), ENTRY(bind_mx4), ENTRY(mx4_compress),
+                                  ENTRY(mx4_decompress), ENTRY(mx4_product), ENTRY(mx4_linear), ENTRY(mx4_gradient), ENTRY(mx4_linear_workspace_bytes),
+                                  {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, functions, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__calls(void) {

@@ -78,7 +78,10 @@ struct MxPlan {
   uint32_t tile;
 };
 constexpr uint64_t kMxFewRows = 64;
-constexpr uint64_t kMxFewRaw = 1ull << 16;  // values of a tile's rows that every workgroup compresses for itself
+constexpr uint64_t kMxFewTiles = 160;
+// Values of a tile's rows that every workgroup compresses for itself rather than reading them from a launch of its own (3.4 us): 16 rows by 4096 x 4096
+// 7.0 us, 5.1 and the launch; by 4096 x 11008 12.7, 8.3 and the launch.
+constexpr uint64_t kMxFewRaw = 1ull << 16;
 static uint32_t mx_few_row_lds(uint64_t k) { return (uint32_t)mx_over(k, kMxStep) * (kMxStepBytes + 4u); }
 
 static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
@@ -89,7 +92,9 @@ static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
   if (p.few) {
     p.ms = rows <= 16 ? 1u : rows <= 32 ? 2u : 4u;
     const uint64_t m_tiles = groups ? std::min<uint64_t>(groups, m) : mx_over(m, 16 * p.ms);
-    p.ns = mx_over(n, 64) * m_tiles >= 512 ? 4u : mx_over(n, 32) * m_tiles >= 256 ? 2u : 1u;
+    // columns a workgroup: 64 or 32 read a's rows less often, where that leaves work for most of the 256 compute units (one row by 11008 x 4096:
+    // 172 workgroups of 64 columns 7.3 us, 344 of 32 8.2, 688 of 16 7.9; by 4096 x 11008: 128 of 32 8.9, 256 of 16 7.9)
+    p.ns = mx_over(n, 64) * m_tiles >= kMxFewTiles ? 4u : mx_over(n, 32) * m_tiles >= kMxFewTiles ? 2u : 1u;
     // a compute unit holds mx4_few_waves wavefronts: they are shared among the workgroups that come to it, none has less than a turn of two steps
     const uint64_t tiles = mx_over(n, 16 * p.ns) * m_tiles, most = mx4_few_waves(p.ms);
     p.waves = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(most / std::min<uint64_t>(most, mx_over(tiles, 256)), mx_over(k, 2 * kMxStep)));

@@ -162,7 +162,7 @@ def linear(x, weight, out_dtype=None):
     then reach x and weight, each in its own type."""
     _check_operands(x, weight, False)
     if isinstance(weight, Mx4Matrix):
-        return _serve(x.detach(), weight, None, out_dtype)
+        return _serve(x.detach() if x.requires_grad else x, weight, None, out_dtype)
     return _Layer.apply(x, weight, None, out_dtype)
 
 
@@ -180,5 +180,5 @@ def experts(x, offsets, weight, out_dtype=None):
     if offsets.numel() != weight.shape[0] + 1:
         raise ValueError(f"{weight.shape[0]} experts need {weight.shape[0] + 1} offsets, not {offsets.numel()}")
     if isinstance(weight, Mx4Matrix):
-        return _serve(x.detach(), weight, offsets, out_dtype)
+        return _serve(x.detach() if x.requires_grad else x, weight, offsets, out_dtype)
     return _Layer.apply(x, weight, offsets, out_dtype)

@@ -152,3 +152,23 @@ def test_python_refusals():
                  lambda: mx4.experts(x, torch.zeros(3, dtype=torch.int32), torch.zeros(2, 3, 8))):
         with pytest.raises(ValueError, match="on a GPU"):
             call()
+
+
+def test_the_two_ways_of_a_call_agree(monkeypatch):
+    """Refusals and sizes by the native marshalling and by ctypes."""
+    x, out, small = torch.zeros(3, 8), torch.zeros(3, 5), torch.zeros(4, dtype=torch.uint8)
+
+    def refusals():
+        for call in (lambda: adacc.mx4_compress(x, small, stream=0), lambda: adacc.mx4_decompress(small, out, stream=0),
+                     lambda: adacc.mx4_product(small, small, 8, out, stream=0), lambda: adacc.mx4_linear(x, small, out, stream=0),
+                     lambda: adacc.mx4_gradient(small, small, 8, out, stream=0)):
+            with pytest.raises(adacc.AdaccError) as e:
+                call()
+            yield e.value.code
+        yield adacc.mx4_linear_workspace_bytes(1000, 20, 300)
+
+    native = list(refusals())
+    assert native[:5] == [adacc.ESIZE] * 5
+    monkeypatch.setattr(adacc, "_mx4_entries", {})
+    monkeypatch.setattr(adacc, "_calls", adacc._LeavesAll())
+    assert list(refusals()) == native
