@@ -36,19 +36,17 @@ __device__ __forceinline__ void mx_store1(void* out, uint32_t type, uint64_t at,
   if (type == kMxF32) static_cast<float*>(out)[at] = v;
   else static_cast<uint16_t*>(out)[at] = (uint16_t)mx_narrow2(type, v, v);
 }
-// N (1, 2 or 4) adjacent values, aligned to their size
+// N (1, 2 or 4) adjacent values, at any element's address (rows of an odd number of values are not aligned)
 template <uint32_t N>
-__device__ __forceinline__ void mx_store(void* out, uint32_t type, uint64_t at, const float (&v)[N]) {
+__device__ __forceinline__ void mx_store(uint8_t* p, uint32_t type, const float (&v)[N]) {
   if constexpr (N == 1) {
-    mx_store1(out, type, at, v[0]);
+    mx_store1(p, type, 0, v[0]);
   } else if (type == kMxF32) {
-    float* p = static_cast<float*>(out) + at;
-    if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    if constexpr (N == 4) *reinterpret_cast<mx_u4u*>(p) = mx_u4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else *reinterpret_cast<mx_u2u*>(p) = mx_u2u{__float_as_uint(v[0]), __float_as_uint(v[1])};
   } else {
-    uint16_t* p = static_cast<uint16_t*>(out) + at;
-    if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = make_uint2(mx_narrow2(type, v[0], v[1]), mx_narrow2(type, v[2], v[3]));
-    else *reinterpret_cast<uint32_t*>(p) = mx_narrow2(type, v[0], v[1]);
+    if constexpr (N == 4) *reinterpret_cast<mx_u2u*>(p) = mx_u2u{mx_narrow2(type, v[0], v[1]), mx_narrow2(type, v[2], v[3])};
+    else *reinterpret_cast<mx_u1u*>(p) = mx_narrow2(type, v[0], v[1]);
   }
 }
 
@@ -318,11 +316,13 @@ __device__ __forceinline__ void mx_tiles(const MxProductArgs& p, uint8_t* lds, N
 
     // results: lane (r, h) holds rows 8 * (e / 4) + 4 * h + e % 4 and column r of a tile
     const uint32_t row0 = w.a_row0 + wm * 32u * SM, col0 = w.b_row0 + wn * 32u * SN;  // of the wavefront
-    const bool aligned = p.vec && w.b_first % 4u == 0u;
-    behind = aligned && w.stride < (1u << 24) && row0 >= w.a_first && row0 + 32u * SM <= w.a_last && col0 >= w.b_first && col0 + 32u * SN <= w.b_last;  // (uniform)
+    const uint32_t size = p.out_type == kMxF32 ? 4u : 2u;
+    const uint32_t high = w.a_last - w.a_first, wide = w.b_last - w.b_first;
+    const uint32_t from_row = row0 - w.a_first, from_col = col0 - w.b_first;  // (beyond the ends, or "negative", at a group's edges)
+    behind = w.stride < (1u << 24) && from_row < high && 32u * SM <= high - from_row && from_col < wide && 32u * SN <= wide - from_col;  // (uniform)
+    const uint64_t down = w.stride * size;
     if (behind) {
-      const uint32_t size = p.out_type == kMxF32 ? 4u : 2u;
-      uint8_t* out = static_cast<uint8_t*>(w.out) + ((uint64_t)(row0 - w.a_first) * w.stride + (col0 - w.b_first)) * size;
+      uint8_t* out = static_cast<uint8_t*>(w.out) + (uint64_t)from_row * down + (uint64_t)from_col * size;
       const uint32_t lane_off = (SM * 4u * h * (uint32_t)w.stride + SN * r) * size;  // (below 2^32: uniform addresses and an offset a lane)
       const auto store_all = [&](auto type) {
         constexpr uint32_t kType = decltype(type)::value;
@@ -330,11 +330,10 @@ __device__ __forceinline__ void mx_tiles(const MxProductArgs& p, uint8_t* lds, N
         for (uint32_t e = 0; e < 16u; ++e) {
 #pragma unroll
           for (uint32_t i = 0; i < SM; ++i) {
-            uint8_t* row = out + (uint64_t)(SM * (8u * (e / 4u) + e % 4u) + i) * w.stride * size;
             float v[SN];
 #pragma unroll
             for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
-            mx_store<SN>(row + lane_off, kType, 0, v);
+            mx_store<SN>(out + (uint64_t)(SM * (8u * (e / 4u) + e % 4u) + i) * down + lane_off, kType, v);
           }
         }
       };
@@ -342,27 +341,42 @@ __device__ __forceinline__ void mx_tiles(const MxProductArgs& p, uint8_t* lds, N
       else if (p.out_type == kMxF16) store_all(std::integral_constant<uint32_t, kMxF16>{});
       else store_all(std::integral_constant<uint32_t, kMxF32>{});
     } else {
-      const uint32_t lane_col = col0 + SN * r;
-      const bool vec = aligned && lane_col + SN <= w.b_last && lane_col >= w.b_first;
-#pragma unroll
-      for (uint32_t i = 0; i < SM; ++i) {
+      // at the edges: rows are looked at one by one, and the columns of a lane that has some inside and some outside
+      const uint32_t lane_col = from_col + SN * r;
+      const bool whole = lane_col < wide && SN <= wide - lane_col;
+      const auto store_some = [&](auto type) {
+        constexpr uint32_t kType = decltype(type)::value;
+        uint32_t row = from_row + SM * 4u * h;
+        uint8_t* at = static_cast<uint8_t*>(w.out) + (int64_t)(int32_t)row * (int64_t)down + (int64_t)(int32_t)lane_col * size;
 #pragma unroll
         for (uint32_t e = 0; e < 16u; ++e) {
-          const uint32_t row = row0 + SM * (8u * (e / 4u) + 4u * h + e % 4u) + i;
-          if (row < w.a_first || row >= w.a_last) continue;
-          const uint64_t at = (uint64_t)(row - w.a_first) * w.stride;
-          float v[SN];
 #pragma unroll
-          for (uint32_t j = 0; j < SN; ++j) v[j] = acc[i][j][e];
-          if (vec) {
-            mx_store<SN>(w.out, p.out_type, at + (lane_col - w.b_first), v);
-          } else {
+          for (uint32_t i = 0; i < SM; ++i) {
+            if (row < high) {
+              float v[SN];
 #pragma unroll
-            for (uint32_t j = 0; j < SN; ++j)
-              if (lane_col + j >= w.b_first && lane_col + j < w.b_last) mx_store1(w.out, p.out_type, at + (lane_col + j - w.b_first), v[j]);
+              for (uint32_t j = 0; j < SN; ++j) {
+                v[j] = acc[i][j][e];
+                asm volatile("" : "+v"(v[j]));  // (or the compiler rounds all values ahead of the branch, for all ways at once)
+              }
+              if (whole) {
+                mx_store<SN>(at, kType, v);
+              } else if constexpr (SN < 4u) {  // (tiles of 256 are only asked for where a lane's columns are all inside or all outside)
+#pragma unroll
+                for (uint32_t j = 0; j < SN; ++j)
+                  if (lane_col + j < wide) mx_store1(at, kType, j, v[j]);
+              }
+            }
+            const uint32_t by = e % 4u == 3u && i == SM - 1u ? 4u * SM + 1u : 1u;
+            row += by;
+            at += by * down;
+            asm volatile("" : "+v"(row), "+v"(at));  // (row after row: 64 addresses at once would not fit in the registers)
           }
         }
-      }
+      };
+      if (p.out_type == kMxBf16) store_some(std::integral_constant<uint32_t, kMxBf16>{});
+      else if (p.out_type == kMxF16) store_some(std::integral_constant<uint32_t, kMxF16>{});
+      else store_some(std::integral_constant<uint32_t, kMxF32>{});
     }
     if (!more) return;
     w = following;
@@ -393,12 +407,13 @@ __device__ __forceinline__ void mx_band(uint32_t id, uint32_t m_tiles, uint32_t 
 template <uint32_t BM, uint32_t BN, uint32_t DEPTH>
 __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_product_kernel(MxProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
-  const uint32_t total = p.m_tiles * p.n_tiles;
+  // p.m_tiles is what there may be at most; numbered by it, the last die would have next to nothing to do
+  const uint32_t m_tiles = min(p.m_tiles, mx_units<true>(p.g, BM)), total = m_tiles * p.n_tiles;
   uint32_t id = blockIdx.x;
   mx_tiles<BM, BN, DEPTH>(p, mx_lds, [&](MxWork& w) {
     for (; id < total; id += gridDim.x) {
       uint32_t mt, nt;
-      mx_band(mx_by_die(id, total), p.m_tiles, p.n_tiles, &mt, &nt);
+      mx_band(mx_by_die(id, total), m_tiles, p.n_tiles, &mt, &nt);
       const MxPlace at = mx_place<true>(p.g, mt, BM);
       const uint32_t a_low = at.first & ~3u;
       if (at.last <= at.first || (uint64_t)at.unit * BM >= (uint64_t)(at.last - a_low)) continue;
@@ -429,11 +444,11 @@ __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kern
   uint32_t id = blockIdx.x;
   mx_tiles<BM, BN, DEPTH>(p, mx_lds, [&](MxWork& w) {
     if (id >= total) return false;
-    const uint32_t at = mx_by_die(id, total);
-    id += gridDim.x;
-    const uint32_t group = at / per;
+    // group by group, every die with a part of each: groups differ in how much there is to do
+    const uint32_t group = id / per;
     uint32_t mt, nt;
-    mx_band(at - group * per, p.m_tiles, p.n_tiles, &mt, &nt);
+    mx_band(mx_by_die(id - group * per, per), p.m_tiles, p.n_tiles, &mt, &nt);
+    id += gridDim.x;
     // steps of the groups before this one, and its own
     const uint32_t lane = threadIdx.x % kWave;
     uint32_t before = 0;

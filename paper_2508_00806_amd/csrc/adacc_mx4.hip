@@ -102,7 +102,7 @@ static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
     return p;
   }
   const auto tiles = [&](uint64_t t) { return mx_over(rows, t) * mx_over(n, t) * std::max<uint32_t>(groups, 1u); };
-  p.tile = tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  p.tile = n % 4 == 0 && tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
   p.ready = true;
   return p;
 }
@@ -139,8 +139,6 @@ static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStr
   a.n_tiles = (uint32_t)mx_over(a.n + (a.g.groups && a.n % 4 ? 3 : 0), plan.tile);
   return mx_launch_tiles(plan.tile, false, m_tiles * a.n_tiles, s, a, "mx4_product_kernel");
 }
-
-static bool mx_vec(const void* out, uint32_t type, uint64_t stride) { return stride % 4 == 0 && !mx_misaligned(out, 4 * mx_size(type)); }
 
 static void mx_compress_args(uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols,
                                     uint64_t row_stride, uint64_t mat_stride, MxCompressArgs* a) {
@@ -269,7 +267,6 @@ static void mx_product_args(const void* b, uint64_t m, uint64_t n, uint64_t k, c
   p->m = (uint32_t)m;
   p->n = (uint32_t)n;
   p->k = (uint32_t)k;
-  p->vec = mx_vec(out, out_type, out_stride);
   p->g.offsets = offsets;
   p->g.groups = groups;
   p->g.rows = (uint32_t)m;
@@ -348,7 +345,6 @@ int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* 
   p.m = (uint32_t)m;
   p.n = (uint32_t)n;
   p.k = (uint32_t)positions;
-  p.vec = mx_vec(out, out_type, out_stride);
   p.g.offsets = offsets;
   p.g.groups = groups;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -358,7 +354,7 @@ int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* 
   }
   p.g.rows = (uint32_t)rows;
   const auto tiles = [&](uint64_t t) { return mx_over(m, t) * mx_over(n, t) * groups; };
-  const uint32_t tile = tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  const uint32_t tile = n % 4 == 0 && tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
   p.m_tiles = (uint32_t)mx_over(m, tile);
   p.n_tiles = (uint32_t)mx_over(n, tile);
   return mx_launch_tiles(tile, true, tiles(tile), s, p, "mx4_gradient_kernel");

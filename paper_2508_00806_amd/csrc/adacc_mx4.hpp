@@ -77,7 +77,6 @@ struct MxProductArgs {
   uint32_t out_type;
   uint32_t m, n;         // rows (of all groups) and columns of the output
   uint32_t m_tiles, n_tiles;
-  uint32_t vec;          // the output's rows start where a lane's columns can be stored at once
   MxGroups g;
   // few rows: the left operand as it is
   const void* x;
@@ -160,6 +159,15 @@ __device__ __forceinline__ MxPlace mx_place(const MxGroups& g, uint32_t unit, ui
   p.first = __builtin_amdgcn_readfirstlane(tail);
   p.last = g.rows;
   return p;
+}
+
+// How many units there are, those of the rows behind the last group included
+template <bool LOWER>
+__device__ __forceinline__ uint32_t mx_units(const MxGroups& g, uint32_t per) {
+  const MxPlace p = mx_place<LOWER>(g, 0xFFFFFFFFu, per);
+  if (g.offsets == nullptr) return (g.rows + per - 1u) / per;
+  const uint32_t from = LOWER ? p.first & ~3u : p.first;
+  return p.before + (p.last > p.first ? (p.last - from + per - 1u) / per : 0u);
 }
 
 typedef uint32_t mx_u4u __attribute__((ext_vector_type(4), aligned(1)));  // loads and stores at any address
