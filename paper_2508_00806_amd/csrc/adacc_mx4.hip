@@ -77,32 +77,41 @@ struct MxPlan {
   uint32_t ms, ns, waves;
   uint32_t tile;
 };
-constexpr uint64_t kMxFewRows = 64;
+constexpr uint64_t kMxCus = 256;
 constexpr uint64_t kMxFewTiles = 160;
 // Values of a tile's rows that every workgroup compresses for itself rather than reading them from a launch of its own (3.4 us): 16 rows by 4096 x 4096
 // 7.0 us, 5.1 and the launch; by 4096 x 11008 12.7, 8.3 and the launch.
 constexpr uint64_t kMxFewRaw = 1ull << 16;
 static uint32_t mx_few_row_lds(uint64_t k) { return (uint32_t)mx_over(k, kMxStep) * (kMxStepBytes + 4u); }
 
+// Rows and columns of a tile, by the number of tiles that there would be.  us in tiles of 256 / 128 / 64: 4096^3 (256, 1024 ... tiles) 38 / 41 / 64;
+// 1024 x 11008 x 4096 (172, 688) 31 / 31 / 45; 1536 x 2048 x 2048 (48, 192, 768) - / 10.9 / 12.0; 1024 x 2048 x 2048 (32, 128, 512) - / 10.2 / 9.8.
+// A tile of 256 has no way for a lane whose four columns are not all inside.
+static uint32_t mx_tile_of(uint64_t rows, uint64_t n, uint64_t live) {
+  const auto tiles = [&](uint64_t t) { return mx_over(rows, t) * mx_over(n, t) * live; };
+  return n % 4 == 0 && tiles(256) >= kMxCus ? 256u : tiles(128) >= 144 ? 128u : 64u;
+}
+
 static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
   MxPlan p;
   std::memset(&p, 0, sizeof p);
   const uint64_t rows = groups ? mx_over(m, groups) : m;  // of a group, on average
-  p.few = rows <= kMxFewRows;
+  const uint64_t live = groups ? std::min<uint64_t>(groups, m) : 1;
+  // 33 to 64 rows: by 11008 x 4096 (172 tiles) 8.9 us in tiles, else 11.7; by 4096 x 4096 (64) 7.7, else 6.1; by 4096 x 11008 16.3, else 12.5
+  p.few = rows <= 32 || (rows <= 64 && mx_over(n, 64) * live < 128);
   if (p.few) {
     p.ms = rows <= 16 ? 1u : rows <= 32 ? 2u : 4u;
-    const uint64_t m_tiles = groups ? std::min<uint64_t>(groups, m) : mx_over(m, 16 * p.ms);
+    const uint64_t m_tiles = groups ? live : mx_over(m, 16 * p.ms);
     // columns a workgroup: 64 or 32 read a's rows less often, where that leaves work for most of the 256 compute units (one row by 11008 x 4096:
     // 172 workgroups of 64 columns 7.3 us, 344 of 32 8.2, 688 of 16 7.9; by 4096 x 11008: 128 of 32 8.9, 256 of 16 7.9)
     p.ns = mx_over(n, 64) * m_tiles >= kMxFewTiles ? 4u : mx_over(n, 32) * m_tiles >= kMxFewTiles ? 2u : 1u;
     // a compute unit holds mx4_few_waves wavefronts: they are shared among the workgroups that come to it, none has less than a turn of two steps
-    const uint64_t tiles = mx_over(n, 16 * p.ns) * m_tiles, most = mx4_few_waves(p.ms);
-    p.waves = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(most / std::min<uint64_t>(most, mx_over(tiles, 256)), mx_over(k, 2 * kMxStep)));
+    const uint64_t wgs = mx_over(n, 16 * p.ns) * m_tiles, most = mx4_few_waves(p.ms);
+    p.waves = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(most / std::min<uint64_t>(most, mx_over(wgs, kMxCus)), mx_over(k, 2 * kMxStep)));
     p.ready = p.ms != 1 || k % 8 != 0 || (groups ? std::min<uint64_t>(m, 16) : m) * k > kMxFewRaw;
     return p;
   }
-  const auto tiles = [&](uint64_t t) { return mx_over(rows, t) * mx_over(n, t) * std::max<uint32_t>(groups, 1u); };
-  p.tile = n % 4 == 0 && tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  p.tile = mx_tile_of(rows, n, live);
   p.ready = true;
   return p;
 }
@@ -118,10 +127,10 @@ static int mx_launch(MxProductFn fn, uint64_t grid, uint32_t threads, uint32_t l
   return launch_check(what);
 }
 
-// As many workgroups as the 256 compute units hold at a time, by LDS: 1, 2 or 4 each
+// As many workgroups as the compute units hold at a time, by LDS: one of tiles of 256, else two
 static int mx_launch_tiles(uint32_t tile, bool gradient, uint64_t tiles, hipStream_t s, const MxProductArgs& a, const char* what) {
   if (tiles > kMxMaxGrid) return ADACC_ELIMIT;
-  const uint64_t room = tile == 256 ? 256 : tile == 128 ? 512 : 1024;
+  const uint64_t room = tile == 256 ? kMxCus : 2 * kMxCus;
   return mx_launch(mx4_product_fn(tile, gradient), std::min(tiles, room), kThreads, mx4_product_lds(tile), s, a, what);
 }
 
@@ -353,11 +362,10 @@ int adacc_mx4_gradient(const void* a, uint64_t a_bytes, uint64_t m, const void* 
     return mx_product(mx_plan(m, n, positions, 0), p, kMxReady, s);
   }
   p.g.rows = (uint32_t)rows;
-  const auto tiles = [&](uint64_t t) { return mx_over(m, t) * mx_over(n, t) * groups; };
-  const uint32_t tile = n % 4 == 0 && tiles(256) >= 256 ? 256u : tiles(128) >= 256 ? 128u : 64u;
+  const uint32_t tile = mx_tile_of(m, n, groups);
   p.m_tiles = (uint32_t)mx_over(m, tile);
   p.n_tiles = (uint32_t)mx_over(n, tile);
-  return mx_launch_tiles(tile, true, tiles(tile), s, p, "mx4_gradient_kernel");
+  return mx_launch_tiles(tile, true, (uint64_t)p.m_tiles * p.n_tiles * groups, s, p, "mx4_gradient_kernel");
 }
 
 }  // extern "C"
