@@ -702,7 +702,7 @@ def _mx4_groups(offsets):
 
 
 def _mx4_blob(blob):
-    return (None, 0) if blob is None else (_ptr(blob), _nbytes(blob))
+    return (None, 0) if blob is None else (blob.data_ptr(), blob.nbytes)
 
 
 def mx4_compress(src, along=None, across=None, offsets=None, scale_rule=MX4_SCALE_FLOOR, stream=None):
@@ -710,15 +710,14 @@ def mx4_compress(src, along=None, across=None, offsets=None, scale_rule=MX4_SCAL
     along: blob of [mats * rows, cols], blocks along the rows; across: blob of [mats * cols, rows] of the transposed matrices, or, with the offsets of
     groups of rows, of [cols, mx4_grouped_cols(rows, groups)].  Either may be None."""
     kind = _mx4_type(src)
-    if src.dim() not in (2, 3) or (src.shape[-1] > 1 and src.stride(-1) != 1):
+    shape, strides = src.shape, src.stride()
+    if len(shape) not in (2, 3) or (strides[-1] != 1 and shape[-1] > 1):
         raise ValueError("src must be a matrix or a stack of matrices with adjacent columns")
-    mats = src.shape[0] if src.dim() == 3 else 1
-    rows, cols = src.shape[-2:]
-    row_stride = src.stride(-2) if rows > 1 else cols
-    mat_stride = src.stride(0) if src.dim() == 3 and mats > 1 else 0
+    mats, mat_stride = (shape[0], strides[0]) if len(shape) == 3 else (1, 0)
+    rows, cols = shape[-2:]
     off, groups = _mx4_groups(offsets)
-    _check(_mx4("mx4_compress")(kind, scale_rule, _ptr(src), mats, rows, cols, row_stride, mat_stride, off, groups, *_mx4_blob(along),
-                                    *_mx4_blob(across), _stream(stream)), "adacc_mx4_compress")
+    _check(_mx4("mx4_compress")(kind, scale_rule, src.data_ptr(), mats, rows, cols, strides[-2] if rows > 1 else cols, mat_stride if mats > 1 else 0,
+                                off, groups, *_mx4_blob(along), *_mx4_blob(across), _stream(stream)), "adacc_mx4_compress")
 
 
 def mx4_decompress(blob, dst, stream=None):

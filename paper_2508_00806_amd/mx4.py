@@ -11,9 +11,11 @@ With MX(.) for the blocks along the rows and MXT(.) for those across them, the g
 
 Plumbing only: buffers and calls; every step runs in the HIP kernels.
 """
+import functools
+
 import torch
 
-from . import (MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE, alloc_mx4, mx4_compress, mx4_decompress, mx4_gradient, mx4_grouped_cols, mx4_linear,
+from . import (MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE, mx4_compress, mx4_decompress, mx4_gradient, mx4_grouped_cols, mx4_layout_of, mx4_linear,
                mx4_linear_workspace_bytes, mx4_product)
 
 SCALE_RULES = {"floor": MX4_SCALE_FLOOR, "fullrange": MX4_SCALE_FULLRANGE}
@@ -69,12 +71,27 @@ def _stack(x):
     return x if plain else x.contiguous()
 
 
+@functools.lru_cache(maxsize=4096)
+def _blob_bytes(rows, cols):
+    return int(mx4_layout_of(rows, cols).total_bytes)
+
+
+@functools.lru_cache(maxsize=4096)
+def _positions(rows, groups):
+    return mx4_grouped_cols(rows, groups)
+
+
+def _buffer(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _blobs(x, along, across, rule, offsets=None):
-    mats = x.shape[0] if x.dim() == 3 else 1
     rows, cols = x.shape[-2:]
-    a = alloc_mx4(mats * rows, cols, device=x.device)[0] if along else None
-    positions = rows if offsets is None else mx4_grouped_cols(rows, offsets.numel() - 1)
-    t = alloc_mx4(mats * cols, positions, device=x.device)[0] if across else None
+    mats = x.shape[0] if x.dim() == 3 else 1
+    a = _buffer(_blob_bytes(mats * rows, cols), x.device) if along else None
+    t = None
+    if across:
+        t = _buffer(_blob_bytes(mats * cols, rows if offsets is None else _positions(rows, offsets.shape[0] - 1)), x.device)
     mx4_compress(x, a, t, offsets=offsets, scale_rule=rule, stream=_stream_of(x))
     return a, t
 
@@ -101,7 +118,7 @@ def _serve(x, w, offsets, out_dtype):
     m = rows.shape[0]
     out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
     need = mx4_linear_workspace_bytes(m, n, k, groups)
-    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    ws = _buffer(need, x.device) if need else None
     mx4_linear(rows, w.blob, out, offsets=offsets, workspace=ws, stream=_stream_of(x))
     return out if x.dim() == 2 else out.view(*x.shape[:-1], n)
 
