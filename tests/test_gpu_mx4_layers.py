@@ -172,3 +172,41 @@ def test_the_saved_form_is_small():
     assert sum(kept) <= 1.001 * 4.25 / 16 * 2 * (x.numel() + w.numel())
     y.sum().backward()
     assert x.grad.shape == x.shape and HALF_STEP[x.dtype] > 0
+
+
+def test_the_example_learns_and_serves():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "mx4_experts.py")
+    spec = importlib.util.spec_from_file_location("mx4_experts_example", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses, err = example.main(["--steps", "12", "--tokens", "512", "--hidden", "256", "--ffn", "512", "--experts", "4"])
+    assert losses[-1] < 0.8 * losses[0]
+    assert err <= 2.0 ** -5  # bf16 sums of values up to 8 in another order
+
+
+@pytest.mark.parametrize("offsets", [[0, 500, 100, -3, 10 ** 9], [7, -1, 2 ** 31 - 1, 0, 64], [0, 300, 300, 299, 300], [300, 300, 300, 300, 300]])
+def test_offsets_without_sense_lead_nowhere(offsets):
+    """Offsets that do not ascend, or lead beyond the rows, are held between 0 and the number of rows: the results mean nothing, and nothing
+    beside them is written."""
+    print(f"[mx4 offsets] {offsets}", flush=True)
+    n, k, rows, groups = 132, 256, 300, 4
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    x, w = matrix(rows, k, torch.bfloat16, 1).cuda(), mx4.compress(matrix(groups * n, k, torch.bfloat16, 2).view(groups, n, k).cuda())
+    for take in (rows, 40):
+        room = torch.full((take + 8, n), 7.0, device="cuda")
+        out = room[4:4 + take]
+        need = adacc.mx4_linear_workspace_bytes(take, n, k, groups)
+        adacc.mx4_linear(x[:take], w.blob, out, offsets=off, workspace=torch.empty(max(need, 256), dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert (room[:4] == 7.0).all() and (room[4 + take:] == 7.0).all()
+    positions = adacc.mx4_grouped_cols(rows, groups)
+    size = int(adacc.mx4_layout_of(k, positions).total_bytes)
+    blob = torch.full((size + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+    adacc.mx4_compress(x, None, blob[256:256 + size], offsets=off)
+    grads = torch.full((groups + 2, k, k), 7.0, device="cuda")
+    adacc.mx4_gradient(blob[256:256 + size], blob[256:256 + size], rows, grads[1:-1], offsets=off)
+    torch.cuda.synchronize()
+    assert (blob[:256] == 0xA5).all() and (blob[256 + size:] == 0xA5).all()
+    assert (grads[0] == 7.0).all() and (grads[-1] == 7.0).all()
