@@ -596,7 +596,9 @@ __global__ __launch_bounds__(mx4_few_waves(MS) * kWave) void mx4_few_kernel(MxPr
   const uint8_t* b_row[NS];
 #pragma unroll
   for (uint32_t j = 0; j < NS; ++j) b_row[j] = p.b.codes + (uint64_t)(b_first + col0 + min(NS * r + j, cols - 1u)) * kMxStepBytes + 16u * q;
-  const uint64_t b_scale_row = min((uint64_t)b_first + col0 + NS * r, p.b.pitch - NS);
+  // NS scale bytes at once, within the block column: those of the stack's last rows, where a matrix begins between two words, are the high ones
+  const uint64_t b_scale_want = (uint64_t)b_first + col0 + NS * r, b_scale_row = min(b_scale_want, p.b.pitch - NS);
+  const uint32_t b_scale_shift = (uint32_t)(b_scale_want - b_scale_row) * 8u % 32u;  // (beyond NS bytes: results that are not kept)
   const uint8_t* b_scale = p.b.scales + (uint64_t)q * p.b.pitch + b_scale_row;
   const uint8_t* a_row[MS];
   const uint8_t* a_scale[MS];
@@ -648,9 +650,10 @@ __global__ __launch_bounds__(mx4_few_waves(MS) * kWave) void mx4_few_kernel(MxPr
 #pragma unroll
     for (uint32_t u = 0; u < U; ++u) {
       if (s0 + u < steps) {  // (uniform)
+        const uint32_t sb = NS > 1u ? t.sb[u] >> b_scale_shift : t.sb[u];
 #pragma unroll
         for (uint32_t i = 0; i < MS; ++i) {
-#define ADACC_MX_AT(J) if constexpr (J < NS) acc[i][J % NS] = mx_mfma16<J>(t.a[u][i], t.b[u][J % NS], acc[i][J % NS], t.sa[u][i], t.sb[u]);
+#define ADACC_MX_AT(J) if constexpr (J < NS) acc[i][J % NS] = mx_mfma16<J>(t.a[u][i], t.b[u][J % NS], acc[i][J % NS], t.sa[u][i], sb);
           ADACC_MX_AT(0) ADACC_MX_AT(1) ADACC_MX_AT(2) ADACC_MX_AT(3)
 #undef ADACC_MX_AT
         }

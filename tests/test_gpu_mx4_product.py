@@ -151,6 +151,22 @@ def test_rows_by_group(offsets, n, k, tail):
         assert (y[offsets[-1]:] == 0).all(), name
 
 
+@pytest.mark.parametrize("groups,n", [(16, 1091), (64, 262), (48, 217), (16, 387), (48, 333), (5, 1003), (3, 2730), (2, 5003), (16, 67), (8, 1030)])
+@pytest.mark.parametrize("each", [1, 11, 40, 150])
+def test_the_last_rows_of_a_stack_whose_matrices_begin_anywhere(groups, n, each):
+    """Matrices of n rows begin between the words of four scale bytes; the last one ends where the block columns do, or shortly before."""
+    print(f"[mx4 groups] {groups} of {each} rows n={n}", flush=True)
+    k, rows = 200, groups * each
+    x, w = matrix(rows, k, torch.bfloat16, 21), matrix(groups * n, k, torch.bfloat16, 22).view(groups, n, k)
+    off = torch.arange(0, rows + 1, each, dtype=torch.int32, device="cuda")
+    stack = mx4.compress(w.cuda())
+    out = torch.full((rows, n), 5.0, device="cuda")
+    adacc.mx4_product(blob_of(x), stack.blob, k, out, offsets=off)
+    for y in (mx4.experts(x.cuda(), off, stack, out_dtype=torch.float32), out):
+        for g in {0, groups // 2, groups - 2, groups - 1}:
+            assert_product(y[g * each:(g + 1) * each], rounded(f64(x))[g * each:(g + 1) * each], rounded(f64(w[g])), torch.float32, sums(k))
+
+
 @pytest.mark.parametrize("offsets", GROUPS, ids=lambda o: f"{len(o) - 1}groups{o[-1]}rows")
 @pytest.mark.parametrize("m,n", [(64, 128), (131, 67), (260, 515)])
 def test_gradient_of_the_groups(offsets, m, n):
