@@ -210,3 +210,34 @@ def test_offsets_without_sense_lead_nowhere(offsets):
     torch.cuda.synchronize()
     assert (blob[:256] == 0xA5).all() and (blob[256 + size:] == 0xA5).all()
     assert (grads[0] == 7.0).all() and (grads[-1] == 7.0).all()
+
+
+def test_more_elements_than_32_bits_count():
+    """A tensor of 4.6e9 elements: both compressions, restorations and products with it, in places on either side of 2^31 and 2^32; results of 4.6e9."""
+    rows, cols = 70001, 65544
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, rows, 10000):
+        x[i:i + 10000].normal_(generator=torch.Generator("cuda").manual_seed(i))
+    along, across = mx4.compress_both(x)
+    print("[mx4 large] compressed", flush=True)
+    y = along.restore(torch.float32)
+    for i in (0, 32764, 32768, 65532, rows - 9):
+        assert np.array_equal(f64(y[i:i + 9]), rounded(f64(x[i:i + 9])))
+    del y
+    y = across.restore(torch.float32)
+    for j in (0, 30677, 30681, 61355, cols - 9):
+        assert np.array_equal(f64(y[j:j + 9]), rounded(f64(x[:, j:j + 9].t().contiguous())))
+    del y, across
+    print("[mx4 large] restored", flush=True)
+    for m in (3, 40, 300):
+        a = matrix(m, cols, torch.bfloat16, m)
+        z = mx4.linear(a.cuda(), along, out_dtype=torch.float32)
+        for i in (0, 32764, 65532, rows - 9):
+            assert_product(z[:, i:i + 9], rounded(f64(a)), rounded(f64(x[i:i + 9])), torch.float32, sums(cols))
+    del x, along, z
+    print("[mx4 large] multiplied", flush=True)
+    a, b = matrix(rows, 64, torch.bfloat16, 41), matrix(cols, 64, torch.bfloat16, 42)
+    z = mx4.linear(a.cuda(), mx4.compress(b.cuda()))
+    bv = rounded(f64(b))
+    for i in (0, 32760, 65530, rows - 9):
+        assert_product(z[i:i + 9], rounded(f64(a[i:i + 9])), bv, torch.bfloat16, sums(64))
