@@ -99,14 +99,14 @@ def _blobs(x, along, across, rule, offsets=None):
 def compress(x, scale_rule="floor"):
     """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension."""
     _on_gpu(x)
-    x = _stack(x.detach())
+    x = _stack(x.detach() if x.requires_grad else x)
     return Mx4Matrix(_blobs(x, True, False, _rule(scale_rule))[0], x.shape)
 
 
 def compress_both(x, scale_rule="floor"):
     """(x, x transposed), both compressed, from one reading of x: blocks along the last dimension, and along the one before it."""
     _on_gpu(x)
-    x = _stack(x.detach())
+    x = _stack(x.detach() if x.requires_grad else x)
     along, across = _blobs(x, True, True, _rule(scale_rule))
     return Mx4Matrix(along, x.shape), Mx4Matrix(across, (*x.shape[:-2], x.shape[-1], x.shape[-2]))
 
