@@ -54,6 +54,10 @@ __device__ __forceinline__ void mx_store(uint8_t* p, uint32_t type, const float 
 // A workgroup of four wavefronts, two by two, takes a tile of BM x BN results, a wavefront SM x SN tiles of 32 x 32 of it.  Codes and scales
 // of a step (128 columns) go to LDS by loads that pass the registers by, DEPTH steps in a ring.
 //
+// What bounds it is power: a step of a tile of 256 takes 1110 to 1180 cycles, 1024 of which are matrix instructions, but on random codes the clock is 1.5 GHz
+// meanwhile (2.4 on zeros).  8192 x 2048 x 8192 takes 63 us, 4.3 PFLOP/s, 16384 x 11008 x 4096 345, 4.3; a launch has 8 to 12 us beside its steps, and
+// the results of a round of tiles (33 MB in 16 bits) are written within 6.
+//
 // Row SM * r + i of a wavefront's rows is row r of its tile i: the SM scale bytes that a lane needs lie side by side, and so do, on the
 // right-hand side, the SN columns of the results that it holds.
 //
@@ -479,7 +483,8 @@ __global__ __launch_bounds__(kThreads, BM == 256 ? 1 : 2) void mx4_gradient_kern
 }
 
 // ------------------------------------------------------------------ few rows
-// What bounds a product of few rows is the reading of b.  A workgroup takes 16 * NS rows of b and up to 16 * MS rows of a; its wavefronts
+// What bounds a product of few rows is the reading of b (one row by 11008 x 4096: 24 MB in 7.3 us, 3.3 TB/s; 64 rows in 32 groups by 2048 x 2048:
+// 72 MB in 14, 5.1).  A workgroup takes 16 * NS rows of b and up to 16 * MS rows of a; its wavefronts
 // share the contraction, U steps at a time in turn, and add their sums up in LDS, in the wavefronts' order.  Codes go from memory to the
 // operand registers: lane (r, q) = (lane % 16, lane / 16) reads block q of the step of its row.  Row NS * r + j of b is row r of
 // tile j, as above.  A turn's loads are under way while the turn before is multiplied, and nothing is loaded under a condition: what is not
