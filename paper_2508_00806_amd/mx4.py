@@ -58,8 +58,8 @@ def _flat(x):
     if x.dim() != 2:
         x = x.reshape(-1, x.shape[-1])
     stride, step = x.stride()
-    cols = x.shape[1]
-    return x if cols <= 1 or (step == 1 and stride >= cols) else x.contiguous()
+    rows, cols = x.shape
+    return x if (step == 1 or cols <= 1) and (stride >= cols or rows <= 1) else x.contiguous()
 
 
 def _stack(x):
@@ -67,7 +67,8 @@ def _stack(x):
         return _flat(x)
     if x.dim() != 3:
         raise ValueError(f"a matrix or a stack of matrices is needed, not {x.dim()} dimensions")
-    plain = x.shape[2] <= 1 or (x.stride(2) == 1 and x.stride(1) >= x.shape[2] and x.stride(0) >= 0)
+    _, rows, cols = x.shape
+    plain = (x.stride(2) == 1 or cols <= 1) and (x.stride(1) >= cols or rows <= 1)
     return x if plain else x.contiguous()
 
 

@@ -1,0 +1,39 @@
+"""mx4 layers whose matrices have one column, or none."""
+import numpy as np
+import pytest
+import torch
+
+from mx4_reference import assert_product, f64, matrix, rounded
+from paper_2508_00806_amd import mx4
+
+pytestmark = pytest.mark.gpu
+
+
+def sums(k):
+    return 2 * (-(-k // 64)) + 10
+
+
+@pytest.mark.parametrize("lead", [(40,), (5, 8), (300,)])
+def test_one_column_of_results_and_the_gradient_of_their_sum(lead):
+    """The gradient of a sum is one value for all rows, no distance apart."""
+    print(f"[mx4 shapes] one column {lead}", flush=True)
+    k, m = 96, int(np.prod(lead))
+    x, w = matrix(m, k, torch.bfloat16, 1, 0.5), matrix(1, k, torch.bfloat16, 2, 0.5)
+    xg, wg = x.cuda().view(*lead, k).requires_grad_(), w.cuda().requires_grad_()
+    y = mx4.linear(xg, wg, out_dtype=torch.float32)
+    y.sum().backward()
+    ones = np.ones((m, 1))
+    assert_product(y.view(m, 1), rounded(f64(x)), rounded(f64(w)), torch.float32, sums(k))
+    assert_product(xg.grad.view(m, k), rounded(ones), rounded(f64(w).T), torch.bfloat16, sums(1))
+    assert_product(wg.grad, rounded(ones.T), rounded(f64(x).T), torch.bfloat16, sums(m))
+
+
+def test_one_broadcast_column_of_rows():
+    print("[mx4 shapes] broadcast column", flush=True)
+    m, n = 70, 33
+    x, w = torch.full((1, 1), 1.5), matrix(n, 1, torch.float32, 3, 0.5)
+    wide = x.cuda().expand(m, 1)
+    for got in (mx4.linear(wide, w.cuda()), mx4.linear(wide, mx4.compress(w.cuda()))):
+        assert_product(got, rounded(f64(x)).repeat(m, 0), rounded(f64(w)), torch.float32, sums(1))
+    stack = mx4.compress(x.cuda().expand(2, m, 1))
+    assert (stack.restore(torch.float32) == 1.5).all() and stack.shape == (2, m, 1)
