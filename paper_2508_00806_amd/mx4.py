@@ -44,7 +44,7 @@ class Mx4Matrix:
         out = torch.empty(self.shape, dtype=dtype, device=self.blob.device) if out is None else out
         if out.shape != self.shape:
             raise ValueError(f"out has shape {tuple(out.shape)}, the matrix {self.shape}")
-        mx4_decompress(self.blob, out if out.dim() == 2 else out.view(-1, self.shape[-1]), stream=_stream_of(self.blob))
+        mx4_decompress(self.blob, out if out.dim() == 2 else out.view(out.shape[:-1].numel(), out.shape[-1]), stream=_stream_of(self.blob))
         return out
 
 
@@ -56,7 +56,7 @@ def _stream_of(t):
 def _flat(x):
     """[..., cols] as a matrix with adjacent columns (a copy only where the strides ask for one)."""
     if x.dim() != 2:
-        x = x.reshape(-1, x.shape[-1])
+        x = x.reshape(x.shape[:-1].numel(), x.shape[-1])  # (not -1: the last dimension may be empty)
     stride, step = x.stride()
     rows, cols = x.shape
     return x if (step == 1 or cols <= 1) and (stride >= cols or rows <= 1) else x.contiguous()

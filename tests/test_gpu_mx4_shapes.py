@@ -37,3 +37,26 @@ def test_one_broadcast_column_of_rows():
         assert_product(got, rounded(f64(x)).repeat(m, 0), rounded(f64(w)), torch.float32, sums(1))
     stack = mx4.compress(x.cuda().expand(2, m, 1))
     assert (stack.restore(torch.float32) == 1.5).all() and stack.shape == (2, m, 1)
+
+
+@pytest.mark.parametrize("lead,n,k", [((2, 3), 5, 0), ((6,), 5, 0), ((2, 3), 0, 8), ((0, 3), 5, 8), ((2, 0), 0, 0)])
+def test_empty_dimensions(lead, n, k):
+    """A contraction of length zero gives zeros; gradients have their shapes."""
+    print(f"[mx4 shapes] empty {lead} {n} {k}", flush=True)
+    x, w = torch.ones(*lead, k, device="cuda", requires_grad=True), torch.ones(n, k, device="cuda", requires_grad=True)
+    held = mx4.compress(w.detach())
+    assert held.restore(torch.float32).shape == (n, k)
+    with torch.no_grad():
+        served = mx4.linear(x, held)
+    y = mx4.linear(x, w)
+    assert served.shape == y.shape == (*lead, n) and torch.equal(served, y.detach())
+    if k == 0:
+        assert (y == 0).all()
+    y.sum().backward()
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape and (w.grad == 0).all()
+
+
+def test_an_empty_stack():
+    for shape in ((3, 4, 0), (3, 0, 8), (0, 4, 8)):
+        along, across = mx4.compress_both(torch.empty(shape, device="cuda"))
+        assert along.restore().shape == shape and across.restore().shape == (shape[0], shape[2], shape[1])

@@ -38,3 +38,21 @@ def test_rows_that_lie_well_are_not_copied():
         assert mx4._flat(x).data_ptr() == x.data_ptr()
     x = torch.zeros(2, 30, 8)[:, ::2, :5]
     assert mx4._stack(x).data_ptr() == x.data_ptr()
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 0), (0, 3, 0), (4, 0), (2, 0, 5), (1, 1, 1, 0), (0,), (7,)])
+def test_empty_dimensions_are_counted(shape):
+    flat = mx4._flat(torch.zeros(shape))
+    rows = 1
+    for d in shape[:-1]:
+        rows *= d
+    assert flat.shape == (rows, shape[-1])
+
+
+@pytest.mark.parametrize("shape", [(3, 4, 0), (0, 4, 0), (3, 0, 8), (3, 0)])
+def test_an_empty_stack_is_restored(shape, monkeypatch):
+    """By the library itself, which touches nothing."""
+    monkeypatch.setattr(mx4, "_stream_of", lambda t: 0)
+    monkeypatch.setattr(mx4, "_on_gpu", lambda t: None)
+    m = mx4.Mx4Matrix(torch.zeros(0, dtype=torch.uint8), shape)
+    assert m.restore(torch.float32).shape == shape
