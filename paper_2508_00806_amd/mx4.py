@@ -41,6 +41,9 @@ class Mx4Matrix:
 
     def restore(self, dtype=torch.bfloat16, out=None):
         """The matrix of the values that the codes stand for."""
+        if _elsewhere(self.blob):
+            with torch.cuda.device(self.blob.get_device()):
+                return self.restore(dtype, out)
         out = torch.empty(self.shape, dtype=dtype, device=self.blob.device) if out is None else out
         if out.shape != self.shape:
             raise ValueError(f"out has shape {tuple(out.shape)}, the matrix {self.shape}")
@@ -51,6 +54,13 @@ class Mx4Matrix:
 def _stream_of(t):
     """The current stream of the tensor's device, as a handle."""
     return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def _elsewhere(t):
+    """Whether another device than the tensor's is current.  A launch goes to the current one (and the default stream has one handle on all of
+    them), so every call makes its tensors' device current; in a backward pass the autograd engine has done so."""
+    at = t.get_device()
+    return at >= 0 and at != torch._C._cuda_getDevice()
 
 
 def _flat(x):
@@ -100,6 +110,9 @@ def _blobs(x, along, across, rule, offsets=None):
 def compress(x, scale_rule="floor"):
     """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension."""
     _on_gpu(x)
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return compress(x, scale_rule)
     x = _stack(x.detach() if x.requires_grad else x)
     return Mx4Matrix(_blobs(x, True, False, _rule(scale_rule))[0], x.shape)
 
@@ -107,6 +120,9 @@ def compress(x, scale_rule="floor"):
 def compress_both(x, scale_rule="floor"):
     """(x, x transposed), both compressed, from one reading of x: blocks along the last dimension, and along the one before it."""
     _on_gpu(x)
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return compress_both(x, scale_rule)
     x = _stack(x.detach() if x.requires_grad else x)
     along, across = _blobs(x, True, True, _rule(scale_rule))
     return Mx4Matrix(along, x.shape), Mx4Matrix(across, (*x.shape[:-2], x.shape[-1], x.shape[-2]))
@@ -179,6 +195,9 @@ def linear(x, weight, out_dtype=None):
     weight: an `Mx4Matrix` (serving: no gradient), or a tensor of bfloat16, float16 or float32, which is compressed by the call; gradients
     then reach x and weight, each in its own type."""
     _check_operands(x, weight, False)
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return linear(x, weight, out_dtype)
     if isinstance(weight, Mx4Matrix):
         return _serve(x.detach() if x.requires_grad else x, weight, None, out_dtype)
     return _Layer.apply(x, weight, None, out_dtype)
@@ -197,6 +216,9 @@ def experts(x, offsets, weight, out_dtype=None):
         raise ValueError("offsets must be on the device of x")
     if offsets.numel() != weight.shape[0] + 1:
         raise ValueError(f"{weight.shape[0]} experts need {weight.shape[0] + 1} offsets, not {offsets.numel()}")
+    if _elsewhere(x):
+        with torch.cuda.device(x.get_device()):
+            return experts(x, offsets, weight, out_dtype)
     if isinstance(weight, Mx4Matrix):
         return _serve(x.detach() if x.requires_grad else x, weight, offsets, out_dtype)
     return _Layer.apply(x, weight, offsets, out_dtype)
