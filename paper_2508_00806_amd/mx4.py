@@ -40,7 +40,10 @@ class Mx4Matrix:
         return self.blob.numel()
 
     def restore(self, dtype=torch.bfloat16, out=None):
-        """The matrix of the values that the codes stand for."""
+        """The matrix of the values that the codes stand for, in a tensor of its own or in `out`, which is of the matrix's shape, on its device."""
+        _on_gpu(self.blob)
+        if out is not None and out.device != self.blob.device:
+            raise ValueError(f"out is on {out.device}, the matrix on {self.blob.device}")
         if _elsewhere(self.blob):
             with torch.cuda.device(self.blob.get_device()):
                 return self.restore(dtype, out)

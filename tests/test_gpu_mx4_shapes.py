@@ -60,3 +60,11 @@ def test_an_empty_stack():
     for shape in ((3, 4, 0), (3, 0, 8), (0, 4, 8)):
         along, across = mx4.compress_both(torch.empty(shape, device="cuda"))
         assert along.restore().shape == shape and across.restore().shape == (shape[0], shape[2], shape[1])
+
+
+def test_restored_into_a_given_tensor():
+    m = mx4.compress(matrix(40, 96, torch.bfloat16, 5).cuda())
+    with pytest.raises(ValueError, match="out is on cpu"):
+        m.restore(out=torch.zeros(40, 96))
+    room = torch.full((40, 100), 7.0, device="cuda")
+    assert m.restore(out=room[:, :96]) is not None and torch.equal(room[:, :96], m.restore(torch.float32)) and (room[:, 96:] == 7.0).all()

@@ -54,3 +54,20 @@ def test_a_current_device_stays_as_it_is(calls, monkeypatch):
     mx4.compress(X)
     mx4.linear(X, W)
     assert len(calls) == 4
+
+
+@pytest.mark.parametrize("blob,out", [("cpu", None), ("cpu", "cpu"), ("meta", "meta")])
+def test_a_matrix_that_is_not_on_a_gpu_is_not_restored(blob, out, monkeypatch):
+    monkeypatch.setattr(mx4, "_stream_of", lambda t: 0)
+    monkeypatch.setattr(mx4, "mx4_decompress", None)  # (no call)
+    m = mx4.Mx4Matrix(torch.zeros(8, dtype=torch.uint8, device=blob), (6, 64))
+    with pytest.raises(ValueError, match="on a GPU"):
+        m.restore(out=None if out is None else torch.zeros(6, 64, device=out))
+
+
+def test_a_matrix_is_restored_on_its_own_device_only(calls):
+    """An address in host memory, or on another device, would reach the kernel."""
+    m = mx4.Mx4Matrix(torch.zeros(8, dtype=torch.uint8), (6, 64))
+    with pytest.raises(ValueError, match="out is on meta"):
+        m.restore(out=torch.zeros(6, 64, device="meta"))
+    assert calls == []
