@@ -190,8 +190,9 @@ template <uint32_t TYPE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void mx4_along_kernel(MxCompressArgs a) {
   using E = MxElem<TYPE, 4>;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const uint32_t ct = blockIdx.x % a.col_tiles;
-  const uint32_t rt = blockIdx.x / a.col_tiles;
+  const uint32_t block = a.first + blockIdx.x;
+  const uint32_t ct = block % a.col_tiles;
+  const uint32_t rt = block / a.col_tiles;
   const uint32_t mat = rt / a.row_tiles;
   const uint32_t row0 = ((rt - mat * a.row_tiles) * kWavesPerWg + wave) * kMxWaveRows;
   if (row0 >= a.rows) return;
@@ -221,8 +222,9 @@ __global__ __launch_bounds__(kThreads, TYPE == kMxF32 ? 2 : 4) void mx4_across_k
   constexpr uint32_t kLaneRoom = V * kMxStepBytes + 16u;
   __shared__ __attribute__((aligned(16))) uint8_t turn[kWave * kLaneRoom];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const uint32_t ct = blockIdx.x % a.col_tiles;
-  const uint32_t rt = blockIdx.x / a.col_tiles;
+  const uint32_t block = a.first + blockIdx.x;
+  const uint32_t ct = block % a.col_tiles;
+  const uint32_t rt = block / a.col_tiles;
   uint32_t mat = 0u, row0, last, step;
   bool across;
   if (a.g.offsets != nullptr) {
@@ -338,8 +340,9 @@ __global__ __launch_bounds__(kThreads) void mx4_restore_kernel(MxDecompressArgs 
   using E = MxElem<TYPE, 4>;
   constexpr uint32_t V = E::V;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const uint32_t ct = blockIdx.x % a.col_tiles;
-  const uint32_t row0 = ((blockIdx.x / a.col_tiles) * kWavesPerWg + wave) * kMxWaveRows;
+  const uint32_t block = a.first + blockIdx.x;
+  const uint32_t ct = block % a.col_tiles;
+  const uint32_t row0 = ((block / a.col_tiles) * kWavesPerWg + wave) * kMxWaveRows;
   const uint32_t col = ct * E::kStrip + lane * V;
   if (row0 >= a.m.rows || col >= a.cols) return;
   const uint32_t rows = min(a.m.rows - row0, kMxWaveRows);

@@ -11,7 +11,8 @@
 namespace adacc {
 
 constexpr uint64_t kMxMaxRows = 1ull << 30;      // of a blob, and columns: kernels count them in 32 bits
-constexpr uint64_t kMxMaxGrid = 0x7FFFFFFFull;
+constexpr uint64_t kMxMaxGrid = 0x7FFFFFFFull;   // workgroups of a call
+constexpr uint64_t kMxMaxThreads = 0xFFFFFFFFull;  // of a launch: the runtime takes fewer than 2^32
 
 static uint64_t mx_align256(uint64_t v) { return (v + 255ull) & ~255ull; }
 static uint64_t mx_over(uint64_t v, uint64_t by) { return (v + by - 1) / by; }
@@ -117,7 +118,7 @@ static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
 }
 
 static int mx_launch(MxProductFn fn, uint64_t grid, uint32_t threads, uint32_t lds, hipStream_t s, const MxProductArgs& a, const char* what) {
-  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  if (grid * threads > kMxMaxThreads) return ADACC_ELIMIT;  // (no product within the limits has so many: tiles 512 workgroups, few rows 2^25 of 64)
   if (grid == 0) return ADACC_OK;
   if (lds > 65536u) {  // more than a launch may ask for unless the kernel has been told (nothing is enqueued by it)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -149,6 +150,20 @@ static int mx_product(const MxPlan& plan, MxProductArgs& a, uint32_t src, hipStr
   return mx_launch_tiles(plan.tile, false, m_tiles * a.n_tiles, s, a, "mx4_product_kernel");
 }
 
+// A conversion: one launch, but for matrices of 2^24 workgroups and more (2^29 rows along, 2^24 matrices across), whose launches follow each other
+template <typename Args>
+static int mx_launch_conversion(void (*fn)(Args), uint64_t grid, hipStream_t s, Args a, const char* what) {
+  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
+  constexpr uint64_t kMost = kMxMaxThreads / kThreads;
+  for (uint64_t at = 0; at < grid; at += kMost) {
+    a.first = (uint32_t)at;
+    hipLaunchKernelGGL(fn, dim3((uint32_t)std::min(grid - at, kMost)), dim3(kThreads), 0, s, a);
+    const int rc = launch_check(what);
+    if (rc != ADACC_OK) return rc;
+  }
+  return ADACC_OK;
+}
+
 static void mx_compress_args(uint32_t scale_rule, const void* src, uint64_t mats, uint64_t rows, uint64_t cols,
                                     uint64_t row_stride, uint64_t mat_stride, MxCompressArgs* a) {
   std::memset(a, 0, sizeof *a);
@@ -170,11 +185,8 @@ static int mx_compress_along(uint32_t type, MxCompressArgs a, void* blob, hipStr
   }
   a.along = mx_matrix(blob, (uint64_t)a.mats * a.rows, a.cols);
   a.row_tiles = (uint32_t)mx_over(a.rows, kMxWaveRows * kWavesPerWg);
-  const uint64_t grid = (uint64_t)a.row_tiles * a.mats * a.col_tiles;
-  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
   const bool narrow = a.cols * mx_size(type) < 16;
-  hipLaunchKernelGGL(mx4_compress_fn(type, true, false, narrow), dim3((uint32_t)grid), dim3(kThreads), 0, s, a);
-  return launch_check("mx4_along_kernel");
+  return mx_launch_conversion(mx4_compress_fn(type, true, false, narrow), (uint64_t)a.row_tiles * a.mats * a.col_tiles, s, a, "mx4_along_kernel");
 }
 
 }  // namespace adacc
@@ -223,11 +235,8 @@ int adacc_mx4_compress(uint32_t type, uint32_t scale_rule, const void* src, uint
   b.g.groups = groups;
   b.col_tiles = (uint32_t)mx_over(cols, 256);
   const uint64_t row_tiles = mx_tiles(rows, groups, kMxTileRows, false);
-  const uint64_t grid = row_tiles * mats * b.col_tiles;
-  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
   b.row_tiles = (uint32_t)row_tiles;
-  hipLaunchKernelGGL(mx4_compress_fn(type, both, true, narrow), dim3((uint32_t)grid), dim3(kThreads), 0, s, b);
-  rc = launch_check("mx4_across_kernel");
+  rc = mx_launch_conversion(mx4_compress_fn(type, both, true, narrow), row_tiles * mats * b.col_tiles, s, b, "mx4_across_kernel");
   if (rc != ADACC_OK || both || !along) return rc;
   return mx_compress_along(type, a, along, s);
 }
@@ -248,10 +257,8 @@ int adacc_mx4_decompress(const void* blob, uint64_t blob_bytes, uint64_t rows, u
   a.dst = dst;
   a.row_stride = row_stride;
   a.col_tiles = (uint32_t)mx_over(cols, type == ADACC_MX4_F32 ? 256 : 512);
-  const uint64_t grid = mx_over(rows, kMxWaveRows * kWavesPerWg) * a.col_tiles;
-  if (grid > kMxMaxGrid) return ADACC_ELIMIT;
-  hipLaunchKernelGGL(mx4_decompress_fn(type), dim3((uint32_t)grid), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), a);
-  return launch_check("mx4_restore_kernel");
+  return mx_launch_conversion(mx4_decompress_fn(type), mx_over(rows, kMxWaveRows * kWavesPerWg) * a.col_tiles, static_cast<hipStream_t>(hip_stream), a,
+                              "mx4_restore_kernel");
 }
 
 // what the three products check alike; the left operand is the caller's matter.  b has the rows of every group.

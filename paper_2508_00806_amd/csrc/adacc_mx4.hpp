@@ -50,6 +50,7 @@ struct MxGroups {
 };
 
 struct MxCompressArgs {
+  uint32_t first;  // workgroup of the call that the launch begins with
   const void* src;
   uint64_t row_stride, mat_stride;  // elements
   uint32_t mats, rows, cols;        // of one matrix; blob rows = mats * rows
@@ -61,6 +62,7 @@ struct MxCompressArgs {
 };
 
 struct MxDecompressArgs {
+  uint32_t first;  // as above
   MxMatrix m;
   uint32_t cols;
   void* dst;
