@@ -80,14 +80,11 @@ struct MxTile {
 
 // 16 (or 4) bytes a lane from base + voff to LDS at `lds` and, lane after lane, behind it.  The counter of vector loads counts it; nothing waits for it
 // but mx_wait_loads (the compiler would wait for all such loads before any read of LDS).
-// m0 holds the address in LDS, as an operand, so that the compiler knows of it.  An SGPR that a vector instruction has written (readfirstlane, or readlane of
-// a spilled one) may be read by a vector load five wait states later, m0 by these loads one later: the compiler does not look into the block to see to
-// it, so the block waits itself.  (Under the matrix instructions it costs nothing.)
 __device__ __forceinline__ void mx_to_lds16(uint32_t lds, const uint8_t* base, uint32_t voff) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(lds), "v"(voff), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
 }
 __device__ __forceinline__ void mx_to_lds4(uint32_t lds, const uint8_t* base, uint32_t voff) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dword %1, %2" : : "{m0}"(lds), "v"(voff), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
 }
 // a pointer that is the same in all lanes, known to be so
 __device__ __forceinline__ const uint8_t* mx_uniform(const uint8_t* p) {
