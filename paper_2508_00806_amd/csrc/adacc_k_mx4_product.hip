@@ -80,11 +80,14 @@ struct MxTile {
 
 // 16 (or 4) bytes a lane from base + voff to LDS at `lds` and, lane after lane, behind it.  The counter of vector loads counts it; nothing waits for it
 // but mx_wait_loads (the compiler would wait for all such loads before any read of LDS).
+// m0 holds the address in LDS; it is an operand, so that the compiler knows of it, and the block waits one state between its write and the load.  A vector
+// load may read an SGPR that a vector instruction has written (readfirstlane, or readlane of a spilled one) five wait states later; the compiler does not look into
+// the block, so tests/test_mx4_instructions.py looks at what it puts ahead of it.  (Five states in the block: 1 % of a product's time.)
 __device__ __forceinline__ void mx_to_lds16(uint32_t lds, const uint8_t* base, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(lds), "v"(voff), "s"(base) : "memory");
 }
 __device__ __forceinline__ void mx_to_lds4(uint32_t lds, const uint8_t* base, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" : : "{m0}"(lds), "v"(voff), "s"(base) : "memory");
 }
 // a pointer that is the same in all lanes, known to be so
 __device__ __forceinline__ const uint8_t* mx_uniform(const uint8_t* p) {
