@@ -14,6 +14,7 @@ Plumbing only: buffers and calls; every step runs in the HIP kernels.
 import functools
 
 import torch
+from torch.autograd import forward_ad
 
 from . import (MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE, mx4_compress, mx4_decompress, mx4_gradient, mx4_grouped_cols, mx4_layout_of, mx4_linear,
                mx4_linear_workspace_bytes, mx4_product)
@@ -111,7 +112,7 @@ def _blobs(x, along, across, rule, offsets=None):
 
 
 def compress(x, scale_rule="floor"):
-    """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension."""
+    """x: a matrix or a stack of matrices of bfloat16, float16 or float32; blocks along the last dimension.  The result is bytes: no gradient passes."""
     _on_gpu(x)
     if _elsewhere(x):
         with torch.cuda.device(x.get_device()):
@@ -141,6 +142,24 @@ def _serve(x, w, offsets, out_dtype):
     ws = _buffer(need, x.device) if need else None
     mx4_linear(rows, w.blob, out, offsets=offsets, workspace=ws, stream=_stream_of(x))
     return out if x.dim() == 2 else out.view(*x.shape[:-1], n)
+
+
+class _Served(torch.autograd.Function):
+    """A product with a kept weight, of rows that a gradient is wanted for.  It has none: the weight's codes have their blocks along the contraction, the
+    gradient of the rows needs them across it.  A backward pass that comes here says so; cut off, the rows would be left without a word."""
+    @staticmethod
+    def forward(ctx, x, w, offsets, out_dtype):
+        return _serve(x, w, offsets, out_dtype)
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise RuntimeError("a product with an Mx4Matrix has no gradient: pass the weight itself to train through it, or detach the rows")
+
+
+def _served(x, w, offsets, out_dtype):
+    if (x.requires_grad and torch.is_grad_enabled()) or forward_ad._current_level >= 0:
+        return _Served.apply(x, w, offsets, out_dtype)
+    return _serve(x, w, offsets, out_dtype)
 
 
 class _Layer(torch.autograd.Function):
@@ -195,14 +214,14 @@ def _check_operands(x, w, mats):
 def linear(x, weight, out_dtype=None):
     """x [..., k] times weight [n, k], both in microscaled 4-bit floating point: [..., n] of x's type, or of out_dtype.
 
-    weight: an `Mx4Matrix` (serving: no gradient), or a tensor of bfloat16, float16 or float32, which is compressed by the call; gradients
+    weight: an `Mx4Matrix` (serving: a backward pass through it raises), or a tensor of bfloat16, float16 or float32, which is compressed by the call; gradients
     then reach x and weight, each in its own type."""
     _check_operands(x, weight, False)
     if _elsewhere(x):
         with torch.cuda.device(x.get_device()):
             return linear(x, weight, out_dtype)
     if isinstance(weight, Mx4Matrix):
-        return _serve(x.detach() if x.requires_grad else x, weight, None, out_dtype)
+        return _served(x, weight, None, out_dtype)
     return _Layer.apply(x, weight, None, out_dtype)
 
 
@@ -211,7 +230,7 @@ def experts(x, offsets, weight, out_dtype=None):
 
     offsets: int32 tensor of experts + 1 entries on x's device; expert e has the rows offsets[e] to offsets[e + 1] (none, if they are equal).  It is
     read on the device, so nothing waits for it.  Rows behind the last expert's give zeros.  weight: an `Mx4Matrix` of shape
-    [experts, n, k], or a tensor of it; gradients as in `linear`."""
+    [experts, n, k], or a tensor of it; gradients, or none, as in `linear`."""
     _check_operands(x, weight, True)
     if x.dim() != 2:
         raise ValueError("x must be a matrix")
@@ -223,5 +242,5 @@ def experts(x, offsets, weight, out_dtype=None):
         with torch.cuda.device(x.get_device()):
             return experts(x, offsets, weight, out_dtype)
     if isinstance(weight, Mx4Matrix):
-        return _serve(x.detach() if x.requires_grad else x, weight, offsets, out_dtype)
+        return _served(x, weight, offsets, out_dtype)
     return _Layer.apply(x, weight, offsets, out_dtype)

@@ -68,3 +68,15 @@ def test_restored_into_a_given_tensor():
         m.restore(out=torch.zeros(40, 96))
     room = torch.full((40, 100), 7.0, device="cuda")
     assert m.restore(out=room[:, :96]) is not None and torch.equal(room[:, :96], m.restore(torch.float32)) and (room[:, 96:] == 7.0).all()
+
+
+def test_rows_that_a_gradient_is_wanted_for_are_served_alike():
+    x, w = matrix(20, 96, torch.bfloat16, 1).cuda(), mx4.compress(matrix(33, 96, torch.bfloat16, 2).cuda())
+    want = mx4.linear(x, w)
+    xg = x.clone().requires_grad_()
+    y = mx4.linear(xg, w)
+    assert torch.equal(y, want)
+    with pytest.raises(RuntimeError, match="Mx4Matrix has no gradient"):
+        y.sum().backward()
+    with torch.no_grad():
+        assert torch.equal(mx4.linear(xg, w), want)
