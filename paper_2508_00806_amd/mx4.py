@@ -14,6 +14,7 @@ Plumbing only: buffers and calls; every step runs in the HIP kernels.
 import functools
 
 import torch
+from torch import _C
 from torch.autograd import forward_ad
 
 from . import (MX4_SCALE_FLOOR, MX4_SCALE_FULLRANGE, mx4_compress, mx4_decompress, mx4_gradient, mx4_grouped_cols, mx4_layout_of, mx4_linear,
@@ -57,14 +58,14 @@ class Mx4Matrix:
 
 def _stream_of(t):
     """The current stream of the tensor's device, as a handle."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+    return _C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _elsewhere(t):
     """Whether another device than the tensor's is current.  A launch goes to the current one (and the default stream has one handle on all of
     them), so every call makes its tensors' device current; in a backward pass the autograd engine has done so."""
     at = t.get_device()
-    return at >= 0 and at != torch._C._cuda_getDevice()
+    return at >= 0 and at != _C._cuda_getDevice()
 
 
 def _flat(x):
@@ -134,9 +135,9 @@ def compress_both(x, scale_rule="floor"):
 
 def _serve(x, w, offsets, out_dtype):
     rows = _flat(x)
-    n, k = w.shape[-2:]
+    m, k = rows.shape
+    n = w.shape[-2]
     groups = 0 if offsets is None else offsets.numel() - 1
-    m = rows.shape[0]
     out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
     need = mx4_linear_workspace_bytes(m, n, k, groups)
     ws = _buffer(need, x.device) if need else None
@@ -202,10 +203,11 @@ def _on_gpu(x):
 
 
 def _check_operands(x, w, mats):
-    if len(w.shape) != (3 if mats else 2):
-        raise ValueError(f"the weight must have {3 if mats else 2} dimensions, not {len(w.shape)}")
-    if x.dim() < 1 or x.shape[-1] != w.shape[-1]:
-        raise ValueError(f"rows of {x.shape[-1] if x.dim() else 0} values do not fit a weight of shape {tuple(w.shape)}")
+    shape, w_shape = x.shape, w.shape
+    if len(w_shape) != (3 if mats else 2):
+        raise ValueError(f"the weight must have {3 if mats else 2} dimensions, not {len(w_shape)}")
+    if not shape or shape[-1] != w_shape[-1]:
+        raise ValueError(f"rows of {shape[-1] if shape else 0} values do not fit a weight of shape {tuple(w_shape)}")
     _on_gpu(x)
     if (w.blob if isinstance(w, Mx4Matrix) else w).get_device() != x.get_device():
         raise ValueError("the weight must be on the device of the rows")
