@@ -317,8 +317,9 @@ int adacc_mask_unpack(const void *bits, uint64_t n, void *mask, void *hip_stream
  *
  * Groups (experts): rows sorted by group; group g has the rows [offsets[g], offsets[g + 1]), any number of them, none included.
  * offsets is DEVICE memory, groups + 1 int32, ascending; offsets[0] counts as 0, rows from offsets[groups] on belong to no group.  The
- * host never reads it.  Offsets that do not ascend or lead beyond the rows give unspecified results, and no access outside of the
- * buffers.  groups = 0, offsets = NULL: no groups.
+ * host never reads it, and chooses a kernel by the rows of a group on average: uneven groups cost about what even ones do.  Offsets that
+ * do not ascend or lead beyond the rows give unspecified results, and no access outside of the buffers.  groups = 0, offsets = NULL:
+ * no groups.
  *
  * Limits (ELIMIT): rows and columns of a blob 2^30, groups 4096.
  * Sizes of zero: ADACC_OK; nothing is touched if there is no result, a contraction of length zero gives zeros. */

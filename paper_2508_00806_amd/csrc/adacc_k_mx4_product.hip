@@ -55,8 +55,9 @@ __device__ __forceinline__ void mx_store(uint8_t* p, uint32_t type, const float 
 // of a step (128 columns) go to LDS by loads that pass the registers by, DEPTH steps in a ring.
 //
 // What bounds it is power: a step of a tile of 256 takes 1110 to 1180 cycles, 1024 of which are matrix instructions, but on random codes the clock is 1.5 GHz
-// meanwhile (2.4 on zeros).  8192 x 2048 x 8192 takes 63 us, 4.3 PFLOP/s, 16384 x 11008 x 4096 345, 4.3; a launch has 8 to 12 us beside its steps, and
-// the results of a round of tiles (33 MB in 16 bits) are written within 6.
+// meanwhile (2.4 on zeros).  8192 x 2048 x 8192 takes 63 us, 4.3 PFLOP/s, 16384 x 11008 x 4096 335 to 350, 4.2 to 4.4: the matrix unit is busy 70 and 57 % of the cycles, but as
+// often a second in both, the clock being 1.4 and 1.7 GHz.  Beside the steps a round of tiles has its ring's start and its results (33 MB in 16 bits, within 6 us; all 361 MB of
+// the second product 77 us, by a contraction of length zero).
 //
 // Row SM * r + i of a wavefront's rows is row r of its tile i: the SM scale bytes that a lane needs lie side by side, and so do, on the
 // right-hand side, the SN columns of the results that it holds.
@@ -377,7 +378,9 @@ __device__ __forceinline__ void mx_tiles(const MxProductArgs& p, uint8_t* lds, N
             const uint32_t by = e % 4u == 3u && i == SM - 1u ? 4u * SM + 1u : 1u;
             row += by;
             at += by * down;
-            asm volatile("" : "+v"(row), "+v"(at));  // (row after row: 64 addresses at once would not fit in the registers)
+            // (row after row: 64 addresses at once would not fit in the registers.  Of a pointer that has gone through here the compiler does not know that it is
+            // global: the stores are flat, and waited for with the next tile's first reads of LDS.  Global ones, by a distance: 16384 rows of 16 groups by 4096 x 2048, 98 us, take 1 us more)
+            asm volatile("" : "+v"(row), "+v"(at));
           }
         }
       };

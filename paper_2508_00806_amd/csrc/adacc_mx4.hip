@@ -98,7 +98,9 @@ static MxPlan mx_plan(uint64_t m, uint64_t n, uint64_t k, uint32_t groups) {
   std::memset(&p, 0, sizeof p);
   const uint64_t rows = groups ? mx_over(m, groups) : m;  // of a group, on average
   const uint64_t live = groups ? std::min<uint64_t>(groups, m) : 1;
-  // 33 to 64 rows: by 11008 x 4096 (172 tiles) 8.9 us in tiles, else 11.7; by 4096 x 4096 (64) 7.7, else 6.1; by 4096 x 11008 16.3, else 12.5
+  // 33 to 64 rows: by 11008 x 4096 (172 tiles) 8.9 us in tiles, else 11.7; by 4096 x 4096 (64) 7.7, else 6.1; by 4096 x 11008 16.3, else 12.5.
+  // 32 rows and fewer, however many tiles: by 11008 x 4096 17 rows 8.4 in tiles, else 8.1; 24 8.4, else 8.3; 32 8.1, else 8.5; by 4096 x 4096 32 rows 7.9, else 4.9
+  // (A group of many rows among groups of few goes the way of the few: 64 groups by 2048 x 2048, all 2048 rows in one, 29 us; 32 in each 34; 9 without groups.)
   p.few = rows <= 32 || (rows <= 64 && mx_over(n, 64) * live < 128);
   if (p.few) {
     p.ms = rows <= 16 ? 1u : rows <= 32 ? 2u : 4u;
