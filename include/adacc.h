@@ -432,7 +432,8 @@ int adacc_act_backward(uint32_t type, uint32_t kind, const void *a, uint64_t a_s
                        void *hip_stream);
 
 /* Products with everything behind them: pre = x w^T + bias (binary32), y = act(pre) + residual.  x [m, k], w [n, k], y and residual [m, n] of `type` (BF16 or F16), bias [n] of that
- * type or F32.  bias, residual: NULL where there is none.  For the backward pass the activation's input can be kept: pre, of `type`, or pre_blob, 8-bit rows of it (before it is rounded).
+ * type or F32.  bias, residual: NULL where there is none.  For the backward pass the activation's input can be kept: pre, of `type` (finite values beyond
+ * that type's range as its largest), or pre_blob, 8-bit rows of it (before it is rounded).
  * workspace: adacc_linear_workspace_bytes(which, m, n, k), which = TRAINED if pre or pre_blob is given, else SERVED. */
 #define ADACC_LINEAR_SERVED 0
 #define ADACC_LINEAR_TRAINED 1

@@ -367,8 +367,10 @@ __device__ __forceinline__ void results_of(const Epilogue& e, const LinResults& 
         keep_codes(e.pre8, at, 32u * P, v);
       } else if (e.pre.at) {
 #pragma unroll
-        for (uint32_t k = 0; k < 16u; ++k)
-          if (32u * P + k < at.rows_left) store_four<TYPE>(e.pre, at.row + 32u * P + k, at, v[k]);
+        for (uint32_t k = 0; k < 16u; ++k) {
+          const float w[4] = {held<TYPE>(v[k][0]), held<TYPE>(v[k][1]), held<TYPE>(v[k][2]), held<TYPE>(v[k][3])};
+          if (32u * P + k < at.rows_left) store_four<TYPE>(e.pre, at.row + 32u * P + k, at, w);
+        }
       }
     }
 #pragma unroll

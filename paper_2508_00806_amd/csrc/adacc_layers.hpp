@@ -174,6 +174,13 @@ __device__ __forceinline__ void store1(void* p, uint64_t at, float v) {
   if constexpr (TYPE == kTypeF32) static_cast<float*>(p)[at] = v;
   else static_cast<uint16_t*>(p)[at] = (uint16_t)narrow2<TYPE>(v, v);
 }
+// What an activation is given, as it is kept in 16 bits: finite values beyond the type's range at its end, where every slope is what it is further out.  (As an infinity, which has no
+// slope, a finite result would have NaN for its gradient.)
+template <uint32_t TYPE>
+__device__ __forceinline__ float held(float v) {
+  constexpr float kMost = TYPE == kTypeF16 ? 65504.0f : 0x1.FEp127f;
+  return __builtin_isfinite(v) ? __builtin_amdgcn_fmed3f(v, -kMost, kMost) : v;
+}
 __device__ __forceinline__ float load1(uint32_t type, const void* p, uint64_t at) {
   return type == kTypeF32 ? load1<kTypeF32>(p, at) : type == kTypeF16 ? load1<kTypeF16>(p, at) : load1<kTypeBf16>(p, at);
 }
@@ -505,8 +512,11 @@ __device__ __forceinline__ void finish(const Epilogue& e, const uint32_t (&row)[
     } else if (e.pre.at) {
 #pragma unroll
       for (uint32_t n = 0; n < N; ++n) {
+        float w[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) w[i] = held<TYPE>(v[n][i]);
         Octet<TYPE> o;
-        o.set(v[n]);
+        o.set(w);
         o.store(e.pre.at, (uint64_t)row[n] * e.pre.stride + col, left[n]);
       }
     }
