@@ -402,23 +402,26 @@ __device__ __forceinline__ void write_group(const Rows8& b, uint32_t row, uint32
 }
 
 // ------------------------------------------------------------------ activations
-// Phi(-|x|), the normal distribution's tail, as a power of two:  2^-P(|x|), P = -log2 Phi(-|x|), which is smooth, as a polynomial fitted on [0, 10].  Its eight coefficients leave 4.7e-7 of
-// gelu itself at most, and 1.9e-5 of the tail where that still counts: for 16-bit types.  Eight products and one exponential: 16 cycles of the vector unit's
-// quarter-rate part where exp(-x^2 / 2) R(1 / (1 + c |x|)) has 32, and a product's results wait for nothing else.
+// Phi(-|x|), the normal distribution's tail, as a power of two:  2^-P(|x|), P = -log2 Phi(-|x|), which is smooth, as a polynomial fitted on [0, 14] for the tail's relative error, which is below
+// 1.9e-5 up to |x| = 6 and below 1.5e-4 beyond, as binary32 evaluates it: a thirteenth of half a step of bfloat16 there, which has such results down to |x| = 13, a twenty-fifth of binary16's,
+// whose results end at 5.7.  (Eight coefficients for [0, 10] gave those of bfloat16 in steps too many: 9 % at -10, 63 % at -12.)  It grows from there on.  Ten products and one exponential: 16 cycles
+// of the vector unit's quarter-rate part where exp(-x^2 / 2) R(1 / (1 + c |x|)) has 32, and a product's results wait for nothing else.
 __device__ __forceinline__ float gelu_tail(float x) {
   const float u = fabsf(x);
-  float p = 1.6465689895994728e-06f;
-  p = fmaf(p, u, -5.7801258662948385e-05f);
-  p = fmaf(p, u, 0.0009012449299916625f);
-  p = fmaf(p, u, -0.008400080725550652f);
-  p = fmaf(p, u, 0.053766608238220215f);
-  p = fmaf(p, u, 0.45861947536468506f);
-  p = fmaf(p, u, 1.1512062549591064f);
-  p = fmaf(p, u, 0.9999980330467224f);
+  float p = 2.0191617267073525e-09f;
+  p = fmaf(p, u, -1.4789505087264843e-07f);
+  p = fmaf(p, u, 4.734183221444255e-06f);
+  p = fmaf(p, u, -8.773975423537195e-05f);
+  p = fmaf(p, u, 0.0010561312083154917f);
+  p = fmaf(p, u, -0.008840742520987988f);
+  p = fmaf(p, u, 0.05443132296204567f);
+  p = fmaf(p, u, 0.4581434428691864f);
+  p = fmaf(p, u, 1.1513323783874512f);
+  p = fmaf(p, u, 0.9999920129776001f);
   return __builtin_amdgcn_exp2f(-p);
 }
 // For binary32: exp(-x^2 / 2) R(t), t = 1 / (1 + c |x|), R = erfcx(|x| / sqrt 2) / 2 as a polynomial without constant term, fitted for the least largest relative error on [0, 40]: 3.9e-7 as
-// binary32 evaluates it.  e: that exponential
+// binary32 evaluates it.  e: that exponential, whose argument's roundings add x^2 2^-23 at most (2.4e-6 of the tail at 4.5, 2e-5 at 13)
 __device__ __forceinline__ float gelu_tail_fine(float x, float e) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.277f, fabsf(x), 1.0f));
   float r = 0.02679574303328991f;
@@ -436,7 +439,7 @@ constexpr float kLog2E = 1.44269504089f;
 constexpr float kTanhTwice = 1.59576912161f;  // 2 sqrt(2 / pi)
 constexpr float kTanhCube = 0.044715f;
 
-// value = x * share, slope = d value / dx
+// value = x * share, slope = d value / dx.  A share below 2^-126 is 0: the exponential and the reciprocal have no results below that.
 template <uint32_t KIND, bool FINE, bool SLOPE>
 __device__ __forceinline__ void activate(float x, float* value, float* slope) {
   if constexpr (KIND == kActNone) {

@@ -46,3 +46,65 @@ def test_a_kept_pre_activation_stays_in_its_types_range(dtype, kind, size):
     y = layers.linear(x, w, b, kind, saved="input")
     kept = [v for v in y.grad_fn.saved_tensors if v is not None][-1]
     assert bool((kept[:, none] == -float("inf")).all()) and bool((kept[:, low] == -most).all())
+
+
+# ---------------------------------------------------------------- small results of activations
+LOWEST = {"gelu": -13.2, "gelu_tanh": -10.5, "silu": -90.0}
+
+
+def tail_bound(kind, x, dtype):
+    """(relative error of share and of what makes the slope) of activations at negative x, by the steps that lead there.
+      gelu, 16 bits: the tail's fit, 1.9e-5 up to 6 and 1.5e-4 beyond, evaluation included, and an exponential
+      gelu, binary32: the fit, 3.9e-7, three roundings of an argument of x^2 / 2, an exponential, four products
+      silu, gelu_tanh: two and eight roundings of an argument z, an exponential, a sum, a reciprocal, a product"""
+    if kind == "gelu":
+        return 2.0 ** -20 + x * x * 2.0 ** -23 if dtype == torch.float32 else torch.where(x.abs() <= 6, 2.0 ** -15, 2.0 ** -12).double()
+    z = x.abs() if kind == "silu" else 1.5957691216 * x.abs() * (1 + 0.044715 * x * x)
+    return 2.0 ** -21 + z * (2.0 ** -23 if kind == "silu" else 2.0 ** -21)
+
+
+def check_tail(kind, x, y, dx, dtype):
+    """Relative to the result, however small it is: half a step of the type and the bound above; shares below 2^-126, and steps below the smallest normal number, count as they are."""
+    x = x.detach().double()
+    value, slope = act(kind, x)
+    z = x.abs() if kind != "gelu_tanh" else 1.5957691216 * x.abs() * (1 + 3 * 0.044715 * x * x)
+    f = torch.finfo(dtype)
+    least, bound = f.smallest_normal * f.eps / 2, tail_bound(kind, x, dtype)
+
+    def within(got, want, size, floor, what):
+        off = (got.detach().double() - want).abs() - f.eps / 2 * want.abs() - bound * size - floor
+        at = int(off.argmax())
+        assert float(off.max()) <= 0, f"{what} at {float(x.flatten()[at])}: {float(got.flatten()[at])} for {float(want.flatten()[at])}"
+    within(y, value, value.abs(), least + 2.0 ** -126 * x.abs(), "y")
+    if dx is not None:
+        share = value / x
+        bound = bound + 2.0 ** -21
+        within(dx, slope, share + (share - slope).abs(), least + 2.0 ** -126 * (2 + z), "dx")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_small_results_of_activations_are_as_exact_as_large_ones(dtype, kind):
+    t = TYPES[dtype]
+    x = torch.linspace(LOWEST[kind], -2.0 ** -6, 97 * 130).view(97, 130).to(t).cuda().requires_grad_()
+    y = layers.activation(x, kind, saved="input")
+    dx, = torch.autograd.grad(y, x, torch.ones_like(y))
+    check_tail(kind, x, y, dx, t)
+    # a gate of them: the product's rounding is the only one more
+    with torch.no_grad():
+        assert torch.equal(layers.gated(x, torch.ones_like(x), kind), y)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("m,n", [(5, 1500), (70, 1500), (3400, 3900)])
+def test_small_results_of_products(m, n, dtype, kind):
+    """Few rows, tiles of 128 and of 256; sums that are one value of w each."""
+    t = TYPES[dtype]
+    w = torch.zeros((n, 40), dtype=t, device="cuda")
+    w[:, 33] = torch.linspace(LOWEST[kind], -2.0 ** -6, n).to(t)
+    x = torch.zeros((m, 40), dtype=t, device="cuda")
+    x[:, 33] = 1
+    y = layers.linear(x, w, activation=kind)
+    assert torch.equal(y, y[:1].expand(m, n))
+    check_tail(kind, w[:, 33], y[0], None, t)
