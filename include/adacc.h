@@ -384,7 +384,7 @@ int adacc_mx4_gradient(const void *a, uint64_t a_bytes, uint64_t m, const void *
  * Outputs must not overlap inputs or each other.
  *
  * 8-bit rows: a row is cut into groups of 128 values from its start, the last one may be short.  M = max|x| of the group, inv = 127 / M (binary32, at most the largest finite
- * number), code = nearest integer of binary32(x * inv), ties to even; S = binary32(M / 127).  Restored value = binary32(S * code), within half of S but for groups below
+ * number), code = nearest integer of binary32(x * inv), ties to even; S = binary32(M / 127), at most the largest number whose 127-fold is finite.  Restored value = binary32(S * code), within half of S but for groups below
  * 2^-119 (within M).  M = 0: zeros.  A group that holds an Inf or NaN restores to NaN.  (Where 128 divides cols, codes and scales are those of an adacc_method of 8 bits, groups of
  * 128, ADACC_SCALE_FULLRANGE and no outliers.)
  * Blob (sections on 256-byte boundaries): codes [rows][pitch], one two's-complement byte a value, pitch = 16 * ceil(cols / 16), unspecified behind the row's end up to there;

@@ -1,9 +1,9 @@
 // The layers whose saved activations are compressed: what the kernels of layer norm, activations and products share with the host code.
 //
 // 8-bit rows: a row is cut into groups of 128 values from its start, the last one may be short.  M = max|x| of a group (binary32), inv = 127 / M held at the
-// largest finite number, code = nearest integer of binary32(x * inv), ties to even, in [-127, 127], S = M / 127.  Restored value = binary32(S * code).
-// M = 0: codes 0, S = 0.  An Inf or NaN in the group: S = NaN, whatever the codes.  (Eq. 2 with the full range of codes, as ADACC_SCALE_FULLRANGE has it: nothing is cut off,
-// every value is within half a step, the scale is one division and so is the inverse.)
+// largest finite number, code = nearest integer of binary32(x * inv), ties to even, in [-127, 127], S = M / 127, or, for an M next to binary32's largest, the largest number
+// whose 127-fold is finite.  Restored value = binary32(S * code).  M = 0: codes 0, S = 0.  An Inf or NaN in the group: S = NaN, whatever the codes.  (Eq. 2 with the full range of codes, as
+// ADACC_SCALE_FULLRANGE has it: nothing is cut off, every value is within half a step but in groups below 2^-119, whose values are within M; the scale is one division and so is the inverse.)
 #pragma once
 
 #include "adacc_common.hpp"
@@ -347,6 +347,7 @@ struct Octet {
 struct Scale8 {
   float scale, inverse;
 };
+constexpr float kScaleMost = 0x1.0204060000000p+121f;  // the largest whose 127-fold is finite
 __device__ __forceinline__ Scale8 scale8(uint32_t most) {
   Scale8 s;
   if (most >= 0x7F800000u) {
@@ -356,7 +357,7 @@ __device__ __forceinline__ Scale8 scale8(uint32_t most) {
     s.scale = s.inverse = 0.0f;
   } else {
     const float m = __uint_as_float(most);
-    s.scale = m / 127.0f;
+    s.scale = fminf(m / 127.0f, kScaleMost);
     s.inverse = fminf(127.0f / m, 3.402823466e38f);
   }
   return s;

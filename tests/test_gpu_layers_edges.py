@@ -108,3 +108,21 @@ def test_small_results_of_products(m, n, dtype, kind):
     y = layers.linear(x, w, activation=kind)
     assert torch.equal(y, y[:1].expand(m, n))
     check_tail(kind, w[:, 33], y[0], None, t)
+
+
+# ---------------------------------------------------------------- groups with the largest numbers
+def test_groups_with_the_largest_binary32_numbers_restore_to_finite_ones():
+    """Half of a scale, and the scale's own rounding 127 times: 0.5001 of it.  (M / 127 rounded up, times 127, would be infinite.)"""
+    most = torch.finfo(torch.float32).max
+    x = rand((5, 300), torch.float32, 1, 1e36)
+    x[0, 7], x[1, 130], x[2, 299] = most, -most, most
+    x[3, 0] = torch.nextafter(torch.tensor(most), torch.tensor(0.0)).item()
+    x[4] = -most
+    back = layers.compress(x).restore(torch.float32)
+    assert bool(torch.isfinite(back).all())
+    scale = torch.nn.functional.pad(x, (0, 84)).unflatten(-1, (3, 128)).abs().amax(-1).double() / 127
+    assert float(((back.double() - x.double()).abs() / scale.repeat_interleave(128, -1)[:, :300]).max()) <= 0.5001
+    x.requires_grad_()
+    for kind in KINDS:  # masks of the type's lowest value, which no gradient reaches
+        dx, = torch.autograd.grad(layers.activation(x, kind), x, torch.ones_like(x))
+        assert bool(torch.isfinite(dx).all()) and not bool(dx[4].any()) and float(dx[1, 130]) == 0 and float(dx[0, 7]) == 1
