@@ -399,30 +399,34 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(NormArgs p) {
 }
 
 // ------------------------------------------------------------------ sums of the workgroups' sums
-// 64 columns a workgroup, sixteen wavefronts that take every sixteenth of the partial sums each
+// 64 columns at a time, sixteen wavefronts that take every sixteenth of the partial sums each.  Workgroups go round where a launch does not take one for every 64 columns.
 __global__ __launch_bounds__(1024) void reduce_kernel(ReduceArgs p) {
   __shared__ float sums[16][kReduceCols];
   const uint32_t lane = threadIdx.x % kReduceCols, wave = threadIdx.x / kReduceCols;
   const uint32_t tiles = (p.cols + kReduceCols - 1u) / kReduceCols;
-  const uint32_t which = blockIdx.x / tiles, col = (blockIdx.x % tiles) * kReduceCols + lane;
-  if (p.out[which] == nullptr) return;
-  float v = 0.0f;
-  if (col < p.cols) {
-    const float* from = p.partial + (uint64_t)which * p.cols + col;
-    const uint64_t apart = (uint64_t)p.parts * p.cols;
-    uint32_t k = wave;
-    for (; k + 48u < p.partials; k += 64u) {
-      const float a = from[k * apart], b = from[(k + 16u) * apart], c = from[(k + 32u) * apart], d = from[(k + 48u) * apart];
-      v += (a + b) + (c + d);
+  for (uint32_t at = blockIdx.x; at < tiles * p.parts; at += gridDim.x) {
+    const uint32_t which = at / tiles, col = (at % tiles) * kReduceCols + lane;
+    if (p.out[which] == nullptr) continue;
+    if (at != blockIdx.x) __syncthreads();  // (the sums of the round before have been read)
+    float v = 0.0f;
+    if (col < p.cols) {
+      const float* from = p.partial + (uint64_t)which * p.cols + col;
+      const uint64_t apart = (uint64_t)p.parts * p.cols;
+      uint32_t k = wave;
+      for (; k + 48u < p.partials; k += 64u) {
+        const float a = from[k * apart], b = from[(k + 16u) * apart], c = from[(k + 32u) * apart], d = from[(k + 48u) * apart];
+        v += (a + b) + (c + d);
+      }
+      for (; k < p.partials; k += 16u) v += from[k * apart];
     }
-    for (; k < p.partials; k += 16u) v += from[k * apart];
-  }
-  sums[wave][lane] = v;
-  __syncthreads();
-  if (wave != 0u || col >= p.cols) return;
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave == 0u && col < p.cols) {
 #pragma unroll
-  for (uint32_t k = 1; k < 16u; ++k) v += sums[k][lane];
-  store1(p.type, p.out[which], col, v);
+      for (uint32_t k = 1; k < 16u; ++k) v += sums[k][lane];
+      store1(p.type, p.out[which], col, v);
+    }
+  }
 }
 ReduceFn reduce_fn() { return reduce_kernel; }
 

@@ -116,7 +116,7 @@ static uint64_t norm_workgroups(NormShape s, bool backward) {
 // Those of the backward pass leave [2][cols] sums each: as many as above, but of fewer than eight rows (or bunches) no more than there are compute units
 static uint32_t norm_partials(uint64_t rows, uint64_t cols) {
   const NormShape s = norm_shape(cols);
-  if (s.octets == 0) return (uint32_t)std::min<uint64_t>(rows, 64);
+  if (s.octets == 0) return (uint32_t)std::min({rows, (uint64_t)64, kLayThreads / kThreads / over(cols, 2048)});  // (a workgroup for 2048 columns of each, in one launch)
   const uint64_t bunches = over(rows, norm_bunch(s));
   return (uint32_t)std::min<uint64_t>(bunches, std::max<uint64_t>(kCus, std::min<uint64_t>(norm_workgroups(s, true), bunches / 8)));
 }
@@ -130,7 +130,7 @@ static int reduce(uint32_t cols, uint32_t partials, uint32_t parts, const float*
   r.partial = partial;
   r.out[0] = a;
   r.out[1] = b;
-  return launch(reduce_fn(), over(cols, kReduceCols) * parts, 1024, 0, s, r, "reduce_kernel");
+  return launch(reduce_fn(), std::min<uint64_t>(over(cols, kReduceCols) * parts, kLayThreads / 1024), 1024, 0, s, r, "reduce_kernel");
 }
 
 // ------------------------------------------------------------------ sums of columns

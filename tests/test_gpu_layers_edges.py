@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import paper_2508_00806_amd as adacc
 from layers_reference import TYPES, act, close, rand
 
 pytestmark = pytest.mark.gpu
@@ -126,3 +127,30 @@ def test_groups_with_the_largest_binary32_numbers_restore_to_finite_ones():
     for kind in KINDS:  # masks of the type's lowest value, which no gradient reaches
         dx, = torch.autograd.grad(layers.activation(x, kind), x, torch.ones_like(x))
         assert bool(torch.isfinite(dx).all()) and not bool(dx[4].any()) and float(dx[1, 130]) == 0 and float(dx[0, 7]) == 1
+
+
+# ---------------------------------------------------------------- sizes near the limits
+def test_parameters_of_more_columns_than_one_launch_sums():
+    """A row of 2^27 + 72 columns: mean and averages are sums of 16385 values a lane, and ten steps between the lanes: within 2^14.1 2^-24 of the sum of the magnitudes."""
+    cols = (1 << 27) + 72
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((1, cols), generator=g, device="cuda", dtype=torch.bfloat16).requires_grad_()
+    w = torch.ones(cols, device="cuda", dtype=torch.bfloat16).requires_grad_()
+    b = torch.zeros(cols, device="cuda", dtype=torch.bfloat16).requires_grad_()
+    dy = torch.randn((1, cols), generator=g, device="cuda", dtype=torch.bfloat16)
+    y = layers.layer_norm(x, w, b, saved="input")
+    dw, db = torch.autograd.grad(y, (w, b), dy)
+    assert torch.equal(db, dy[0])
+    off = 2.0 ** -9.8
+    for part in (slice(0, 1 << 20), slice(cols - (1 << 20), cols)):
+        v, d = x.detach()[0, part].double(), dy[0, part].double()  # mean 0 and deviation 1, within 2^-12 of them
+        close(dw[part], d * v, torch.bfloat16, off * d.abs() * (1 + v.abs()), "dw")
+        close(y.detach()[0, part], v, torch.bfloat16, off * (1 + v.abs()), "y")
+
+
+def test_a_bias_of_more_columns_than_one_launch_sums():
+    n = (1 << 28) + 72
+    dy = torch.randn((1, n), device="cuda", dtype=torch.bfloat16)
+    db = torch.empty(n, device="cuda", dtype=torch.bfloat16)
+    adacc.linear_columns(dy, dbias=db, workspace=torch.empty(adacc.linear_columns_workspace_bytes(1, n), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(db, dy[0])

@@ -1,0 +1,29 @@
+"""Calls at the limits of the layers' sizes; no GPU is needed, and none may be there: what is taken would be launched on addresses that do not exist, and fails where there is no GPU."""
+import pytest
+import torch
+
+import paper_2508_00806_amd as adacc
+from test_layers_host import BIG, CALLS, P
+
+EHIP, ELIMIT = adacc.EHIP, adacc.ELIMIT
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="the call would be launched")
+
+
+def call(name, **change):
+    return getattr(adacc.lib(), "adacc_" + name)(*{**CALLS[name], **change}.values())
+
+
+@no_gpu
+@pytest.mark.parametrize("cols", [1 << 27, (1 << 28) + 1, 1 << 30])
+def test_sums_of_columns_of_any_number_are_taken(cols):
+    """(Of no rows: the sums' launch is the only one.)"""
+    assert call("norm_backward", rows=0, cols=cols, dx=None) == EHIP
+    assert call("norm_backward", rows=0, cols=cols, dx=None, dweight=None) == EHIP
+    assert call("linear_columns", m=0, n=cols) == EHIP
+
+
+def test_the_first_launch_of_many_wide_rows_is_taken():
+    """A workgroup for 2048 columns of each of the partial sums, fewer than 2^32 threads in all."""
+    for rows, cols in ((32, 1 << 30), (64, 1 << 29), (1 << 20, (1 << 30) - 5)):
+        partials = adacc.norm_workspace_bytes(rows, cols) // (8 * cols)
+        assert 1 <= partials <= 64 and partials * -(-cols // 2048) * 256 < 1 << 32
