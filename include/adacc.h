@@ -380,7 +380,7 @@ int adacc_mx4_gradient(const void *a, uint64_t a_bytes, uint64_t m, const void *
  * Each call is a layer's own pass with the compression in it: what the backward pass needs is written while the input is read for the result, and read in that form
  * by the gradient's kernel.  Types are ADACC_MX4_BF16 / _F16 / _F32; results are rounded once, to nearest even; sums are binary32, in an order that depends on
  * the sizes alone.  Matrices are [rows, cols] with adjacent columns, any number of elements between rows, at any element's address.  Limits (ELIMIT): rows and columns
- * 2^30; for the operands of products fewer than 2^23 elements between rows.  Sizes of zero: ADACC_OK; no result, nothing is touched; sums over nothing are zeros.
+ * 2^30; for activations and 8-bit rows by themselves 2^30 groups of 128 in all rows; for the operands of products fewer than 2^23 elements between rows.  Sizes of zero: ADACC_OK; no result, nothing is touched; sums over nothing are zeros.
  * Outputs must not overlap inputs or each other.
  *
  * 8-bit rows: a row is cut into groups of 128 values from its start, the last one may be short.  M = max|x| of the group, inv = 127 / M (binary32, at most the largest finite

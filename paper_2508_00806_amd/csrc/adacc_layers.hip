@@ -12,6 +12,7 @@ namespace adacc {
 
 constexpr uint64_t kLayMost = 1ull << 30;         // rows and columns of a matrix: kernels count them in 32 bits
 constexpr uint64_t kLayThreads = 0xFFFFFFFFull;   // of a launch: the runtime takes fewer than 2^32
+constexpr uint64_t kLayGroupsMost = 1ull << 30;   // groups of 128 in all rows of a call of the kernels that have sixteen lanes for each
 constexpr uint64_t kLinStrideMost = 1ull << 23;   // elements between the rows of a product's operands: a tile's offsets have 32 bits
 constexpr uint64_t kCus = 256;
 
@@ -20,6 +21,7 @@ static uint64_t over(uint64_t v, uint64_t by) { return (v + by - 1) / by; }
 static bool lay_misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 static uint64_t lay_size(uint32_t type) { return type == kTypeF32 ? 4u : 2u; }
 static bool lay_sizes_ok(uint64_t rows, uint64_t cols) { return rows <= kLayMost && cols <= kLayMost; }
+static bool lay_groups_ok(uint64_t rows, uint64_t cols) { return lay_sizes_ok(rows, cols) && rows * over(cols, kR8Group) <= kLayGroupsMost; }
 
 static void rows8_layout(uint64_t rows, uint64_t cols, adacc_rows8_layout* L) {
   L->pitch = over(cols, 16) * 16;
@@ -89,11 +91,28 @@ static int launch(void (*fn)(Args), uint64_t grid, uint32_t threads, uint32_t ld
 
 // groups of 128 columns, 16 lanes each, kR8Units one after the other a lane
 static uint64_t group_grid(uint64_t rows, uint64_t cols) { return over(rows * over(cols, kR8Group), (kThreads / kR8Lanes) * kR8Units); }
-template <typename Args>
-static void group_steps(Args* a) {
-  const uint32_t groups = (uint32_t)over(a->cols, kR8Group), step = kThreads / kR8Lanes;
-  a->step_rows = step / groups;
-  a->step_groups = step % groups;
+// ... as many rows at a time as a launch takes; behind(a, n): a's matrices begin n rows further on
+template <typename Args, typename Behind>
+static int launch_groups(void (*fn)(Args), uint64_t rows, Args a, hipStream_t s, const char* what, Behind&& behind) {
+  const uint32_t groups = (uint32_t)over(a.cols, kR8Group), step = kThreads / kR8Lanes;
+  a.step_rows = step / groups;
+  a.step_groups = step % groups;
+  const uint64_t most = kLayThreads / kThreads * (step * kR8Units) / groups;
+  for (uint64_t at = 0; at < rows; at += most) {
+    const uint64_t now = std::min(rows - at, most);
+    a.rows = (uint32_t)now;
+    ADACC_TRY(launch(fn, group_grid(now, a.cols), (uint32_t)kThreads, 0, s, a, what));
+    behind(&a, now);
+  }
+  return ADACC_OK;
+}
+
+static auto act_behind(uint32_t type) {
+  return [type](ActArgs* p, uint64_t n) {
+    for (Strided* m : {&p->a, &p->up, &p->y, &p->da, &p->dup}) skip(m, n, type);
+    skip(&p->a8, n);
+    skip(&p->up8, n);
+  };
 }
 
 // ------------------------------------------------------------------ layer norm
@@ -275,17 +294,18 @@ int adacc_rows8_layout_of(uint64_t rows, uint64_t cols, adacc_rows8_layout* out)
 
 static int rows8_call(bool restore, uint32_t type, const void* m, uint64_t rows, uint64_t cols, uint64_t stride, const void* blob, uint64_t blob_bytes, void* hip_stream) {
   if (type > kTypeF32) return ADACC_EINVAL;
-  if (!lay_sizes_ok(rows, cols)) return ADACC_ELIMIT;
+  if (!lay_groups_ok(rows, cols)) return ADACC_ELIMIT;
   if (!rows || !cols) return ADACC_OK;
   ADACC_TRY(check_matrix(m, type, rows, cols, stride));
   ADACC_TRY(check_blob(blob, blob_bytes, rows, cols));
   Rows8Args a;
-  a.rows = (uint32_t)rows;
   a.cols = (uint32_t)cols;
   a.m = strided(m, stride);
   a.blob = rows8_of(blob, rows, cols);
-  group_steps(&a);
-  return launch(restore ? rows8_restore_fn(type) : rows8_compress_fn(type), group_grid(rows, cols), (uint32_t)kThreads, 0, static_cast<hipStream_t>(hip_stream), a, "rows8_kernel");
+  return launch_groups(restore ? rows8_restore_fn(type) : rows8_compress_fn(type), rows, a, static_cast<hipStream_t>(hip_stream), "rows8_kernel", [type](Rows8Args* p, uint64_t n) {
+    skip(&p->m, n, type);
+    skip(&p->blob, n);
+  });
 }
 int adacc_rows8_compress(uint32_t type, const void* src, uint64_t rows, uint64_t cols, uint64_t row_stride, void* blob, uint64_t blob_bytes, void* hip_stream) {
   return rows8_call(false, type, src, rows, cols, row_stride, blob, blob_bytes, hip_stream);
@@ -407,7 +427,7 @@ int adacc_act_forward(uint32_t type, uint32_t kind, const void* a, uint64_t a_st
                       uint64_t a_blob_bytes, void* up_blob, uint64_t up_blob_bytes, void* hip_stream) {
   if (type > kTypeF32 || kind < kActGelu || kind > kActSilu) return ADACC_EINVAL;
   if ((up_blob != nullptr) != (up && a_blob)) return ADACC_EINVAL;
-  if (!lay_sizes_ok(rows, cols)) return ADACC_ELIMIT;
+  if (!lay_groups_ok(rows, cols)) return ADACC_ELIMIT;
   if (!rows || !cols) return ADACC_OK;
   ADACC_TRY(check_matrix(a, type, rows, cols, a_stride));
   if (up) ADACC_TRY(check_matrix(up, type, rows, cols, up_stride));
@@ -416,15 +436,13 @@ int adacc_act_forward(uint32_t type, uint32_t kind, const void* a, uint64_t a_st
   if (up_blob) ADACC_TRY(check_blob(up_blob, up_blob_bytes, rows, cols));
   ActArgs p;
   std::memset(&p, 0, sizeof p);
-  p.rows = (uint32_t)rows;
   p.cols = (uint32_t)cols;
   p.a = strided(a, a_stride);
   p.up = strided(up, up_stride);
   p.y = strided(y, y_stride);
   p.a8 = rows8_of(a_blob, rows, cols);
   p.up8 = rows8_of(up_blob, rows, cols);
-  group_steps(&p);
-  return launch(act_forward_fn(type, kind, up != nullptr, a_blob != nullptr, cols % 8 == 0), group_grid(rows, cols), (uint32_t)kThreads, 0, static_cast<hipStream_t>(hip_stream), p, "act_forward_kernel");
+  return launch_groups(act_forward_fn(type, kind, up != nullptr, a_blob != nullptr, cols % 8 == 0), rows, p, static_cast<hipStream_t>(hip_stream), "act_forward_kernel", act_behind(type));
 }
 
 int adacc_act_backward(uint32_t type, uint32_t kind, const void* a, uint64_t a_stride, const void* a_blob, uint64_t a_blob_bytes, const void* up, uint64_t up_stride, const void* up_blob,
@@ -433,7 +451,7 @@ int adacc_act_backward(uint32_t type, uint32_t kind, const void* a, uint64_t a_s
   if ((a && a_blob) || (up && up_blob) || (up && a_blob) || (up_blob && a)) return ADACC_EINVAL;
   const bool gated = up || up_blob;
   if (dup && !gated) return ADACC_EINVAL;
-  if (!lay_sizes_ok(rows, cols)) return ADACC_ELIMIT;
+  if (!lay_groups_ok(rows, cols)) return ADACC_ELIMIT;
   if (!rows || !cols || (!da && !dup)) return ADACC_OK;
   if (a_blob) ADACC_TRY(check_blob(a_blob, a_blob_bytes, rows, cols));
   else ADACC_TRY(check_matrix(a, type, rows, cols, a_stride));
@@ -444,7 +462,6 @@ int adacc_act_backward(uint32_t type, uint32_t kind, const void* a, uint64_t a_s
   if (dup) ADACC_TRY(check_matrix(dup, type, rows, cols, dup_stride));
   ActArgs p;
   std::memset(&p, 0, sizeof p);
-  p.rows = (uint32_t)rows;
   p.cols = (uint32_t)cols;
   p.a = strided(a, a_stride);
   p.up = strided(up, up_stride);
@@ -453,8 +470,7 @@ int adacc_act_backward(uint32_t type, uint32_t kind, const void* a, uint64_t a_s
   p.dup = strided(dup, dup_stride);
   p.a8 = rows8_of(a_blob, rows, cols);
   p.up8 = rows8_of(up_blob, rows, cols);
-  group_steps(&p);
-  return launch(act_backward_fn(type, kind, gated, a_blob != nullptr, cols % 8 == 0), group_grid(rows, cols), (uint32_t)kThreads, 0, static_cast<hipStream_t>(hip_stream), p, "act_backward_kernel");
+  return launch_groups(act_backward_fn(type, kind, gated, a_blob != nullptr, cols % 8 == 0), rows, p, static_cast<hipStream_t>(hip_stream), "act_backward_kernel", act_behind(type));
 }
 
 // ------------------------------------------------------------------ products

@@ -154,3 +154,22 @@ def test_a_bias_of_more_columns_than_one_launch_sums():
     db = torch.empty(n, device="cuda", dtype=torch.bfloat16)
     adacc.linear_columns(dy, dbias=db, workspace=torch.empty(adacc.linear_columns_workspace_bytes(1, n), dtype=torch.uint8, device="cuda"))
     assert torch.equal(db, dy[0])
+
+
+def test_as_many_rows_as_there_may_be():
+    """2^30 rows of one value, which take two launches: what the same values in rows of 2^15 give."""
+    rows = 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty((rows, 1), device="cuda", dtype=torch.bfloat16)
+    x.view(-1, 1 << 24)[:] = torch.randn((1 << 6, 1 << 24), generator=g, device="cuda", dtype=torch.bfloat16)
+    wide = x.view(1 << 15, 1 << 15)
+    assert torch.equal(layers.activation(x).view_as(wide), layers.activation(wide))
+    grads = []
+    for v in (x, wide):
+        v = v.detach().requires_grad_()
+        grads.append(torch.autograd.grad(layers.activation(v, "silu", saved="input"), v, x.view_as(v))[0])
+    assert torch.equal(grads[0].view_as(wide), grads[1])
+    del grads
+    kept = layers.compress(x)  # (a group of one value: its code is 127, with the value's sign)
+    back = kept.restore(torch.bfloat16)
+    assert torch.equal(back, x)

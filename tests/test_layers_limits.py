@@ -27,3 +27,21 @@ def test_the_first_launch_of_many_wide_rows_is_taken():
     for rows, cols in ((32, 1 << 30), (64, 1 << 29), (1 << 20, (1 << 30) - 5)):
         partials = adacc.norm_workspace_bytes(rows, cols) // (8 * cols)
         assert 1 <= partials <= 64 and partials * -(-cols // 2048) * 256 < 1 << 32
+
+
+@no_gpu
+@pytest.mark.parametrize("rows,cols", [(1 << 30, 1), (1 << 29, 200), ((1 << 30) - 3, 100), (1, 1 << 30)])
+def test_as_many_groups_as_the_limit_says_are_taken(rows, cols):
+    given = dict(rows=rows, cols=cols)
+    assert call("rows8_compress", stride=cols, **given) == EHIP
+    assert call("rows8_decompress", stride=cols, **given) == EHIP
+    assert call("act_forward", a_stride=cols, up_stride=cols, y_stride=cols, **given) == EHIP
+    assert call("act_backward", dy_stride=cols, da_stride=cols, dup_stride=cols, **given) == EHIP
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 30, 129), ((1 << 23) + 1, 128 * 128)])
+def test_more_groups_are_refused(rows, cols):
+    given = dict(rows=rows, cols=cols)
+    assert call("rows8_compress", stride=cols, **given) == call("rows8_decompress", stride=cols, **given) == ELIMIT
+    assert call("act_forward", a_stride=cols, up_stride=cols, y_stride=cols, **given) == ELIMIT
+    assert call("act_backward", dy_stride=cols, da_stride=cols, dup_stride=cols, **given) == ELIMIT
