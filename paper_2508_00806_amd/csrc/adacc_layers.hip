@@ -586,7 +586,7 @@ int adacc_linear_weight_gradient(uint32_t type, const void* dpre, uint64_t dpre_
     ADACC_TRY(check_operand(dpre, m, n, dpre_stride));
     if (x_blob) ADACC_TRY(check_blob(x_blob, x_blob_bytes, m, k));
     else ADACC_TRY(check_operand(x, m, k, x_stride));
-    if (x_blob && k >= kLinStrideMost) return ADACC_ELIMIT;
+    if (x_blob && m > 1 && k >= kLinStrideMost) return ADACC_ELIMIT;
   }
   ADACC_TRY(check_matrix(dw, type, n, k, dw_stride));
   ADACC_TRY(check_workspace(workspace, workspace_bytes, adacc_linear_workspace_bytes(ADACC_LINEAR_WEIGHT_GRADIENT, m, n, k)));

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2508_00806_amd as adacc
-from layers_reference import TYPES, act, close, rand
+from layers_reference import TYPES, act, close, groups, rand
 
 pytestmark = pytest.mark.gpu
 layers = pytest.importorskip("paper_2508_00806_amd.layers")
@@ -173,3 +173,24 @@ def test_as_many_rows_as_there_may_be():
     kept = layers.compress(x)  # (a group of one value: its code is 127, with the value's sign)
     back = kept.restore(torch.bfloat16)
     assert torch.equal(back, x)
+
+
+@pytest.mark.parametrize("saved", ["codes", "input"])
+def test_a_product_of_one_row_longer_than_rows_may_lie_apart(saved):
+    """One row by one row of 2^23 + 77 values.  The result: a sum of k products, (k + 8) 2^-24 of the magnitudes at most; dx and dw: one product each, of dpre rounded to its type."""
+    k = (1 << 23) + 77
+    x, w = rand((1, k), torch.bfloat16, 1), rand((1, k), torch.bfloat16, 2, 2.0 ** -12)
+    leaves = [t.requires_grad_() for t in (x, w)]
+    y = layers.linear(x, w, activation="silu", saved=saved)
+    dy = torch.full((1, 1), 0.5, dtype=torch.bfloat16, device="cuda")
+    kept = [t for t in y.grad_fn.saved_tensors if t is not None][-1]
+    pre = layers.Rows8(kept, (1, 1)).restore(torch.float32).double() if saved == "codes" else kept.double()
+    dx, dw = torch.autograd.grad(y, leaves, dy)
+    X, W = x.detach().double(), w.detach().double()
+    exact, size = (X * W).sum(), (X * W).abs().sum()
+    assert float((pre - exact).abs()) <= float((k + 8) * 2.0 ** -24 * size + exact.abs() * 2.0 ** -7)
+    dpre = 0.5 * act("silu", pre)[1]
+    near = torch.finfo(torch.bfloat16).eps / 2 + E
+    restored = groups(x.detach())[2].bfloat16().double() if saved == "codes" else X
+    close(dx, dpre * W, torch.bfloat16, near * (dpre * W).abs() + E * W.abs() * (1 + pre.abs()), "dx")
+    close(dw, dpre * restored, torch.bfloat16, near * (dpre * restored).abs() + E * restored.abs() * (1 + pre.abs()), "dw")

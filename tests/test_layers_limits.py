@@ -45,3 +45,11 @@ def test_more_groups_are_refused(rows, cols):
     assert call("rows8_compress", stride=cols, **given) == call("rows8_decompress", stride=cols, **given) == ELIMIT
     assert call("act_forward", a_stride=cols, up_stride=cols, y_stride=cols, **given) == ELIMIT
     assert call("act_backward", dy_stride=cols, da_stride=cols, dup_stride=cols, **given) == ELIMIT
+
+
+@no_gpu
+@pytest.mark.parametrize("k", [1 << 23, 1 << 30])
+def test_a_weights_gradient_from_one_row_of_any_length_is_taken(k):
+    """From codes as from the row itself: no other row lies behind it."""
+    wide = dict(m=1, n=1, k=k, d_stride=1, dw_stride=k)
+    assert call("linear_weight_gradient", **wide) == call("linear_weight_gradient", x=P, x_stride=k, x_blob=None, **wide) == EHIP
