@@ -194,7 +194,8 @@ static LinPlan lin_plan(uint64_t m, uint64_t n, uint64_t k, bool may_be_few) {
     // columns of a workgroup: 64 read x less often, which 17 rows and more gain by where workgroups enough are left (32 by 11008 x 4096: 29 us, of 16 columns 35; by 4096 x 4096 25 and 12)
     p.ns = p.ms == 2 && over(n, 64) >= 160 ? 4u : 1u;
     p.waves = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kFewWaves, over(k, 4 * 32)));
-    return p;
+    if (over(n, 16 * p.ns) * p.waves * kWave <= kLayThreads) return p;  // (a launch's; tiles are taken in turn)
+    p.few = false;
   }
   const uint64_t steps = over(k, kLinStep);
   p.tile = 128u;
@@ -243,6 +244,8 @@ static int product(const LinPlan& plan, uint32_t type, LinOperand a, uint32_t a_
   std::memset(&p, 0, sizeof p);
   p.e = e;
   p.k = (uint32_t)k;
+  const uint64_t total = plan.few ? 0 : over(e.m, plan.tile) * over(e.n, plan.tile) * plan.splits;
+  if (total > 0x7FFFFFFFull) return ADACC_ELIMIT;
   if (plan.few) {
     p.a = strided(a.at, a.stride);
     p.b = strided(b.at, b.stride);
@@ -261,8 +264,6 @@ static int product(const LinPlan& plan, uint32_t type, LinOperand a, uint32_t a_
   p.splits = plan.splits;
   p.split_steps = plan.split_steps;
   p.partial = reinterpret_cast<float*>(ws);
-  const uint64_t total = (uint64_t)p.m_tiles * p.n_tiles * p.splits;
-  if (total > 0x7FFFFFFFull) return ADACC_ELIMIT;
   const uint64_t room = plan.tile == 256 ? kCus : 2 * kCus;  // as many workgroups as the compute units hold at a time, by LDS
   ADACC_TRY(launch(product_fn(type, a_mode, b_mode, plan.tile), std::min(total, room), (uint32_t)kThreads, product_lds(plan.tile), s, p, "lin_product_kernel"));
   if (plan.splits == 1) return ADACC_OK;

@@ -194,3 +194,13 @@ def test_a_product_of_one_row_longer_than_rows_may_lie_apart(saved):
     restored = groups(x.detach())[2].bfloat16().double() if saved == "codes" else X
     close(dx, dpre * W, torch.bfloat16, near * (dpre * W).abs() + E * W.abs() * (1 + pre.abs()), "dx")
     close(dw, dpre * restored, torch.bfloat16, near * (dpre * restored).abs() + E * restored.abs() * (1 + pre.abs()), "dw")
+
+
+def test_one_row_by_as_many_as_there_may_be():
+    n = 1 << 30
+    w = torch.zeros((n, 8), dtype=torch.bfloat16, device="cuda")
+    w[:, 5] = (torch.arange(n, device="cuda") % 251).bfloat16()
+    x = torch.tensor([[7.0, 0, 0, 0, 0, 3.0, 0, 1.0]], dtype=torch.bfloat16, device="cuda")
+    y = layers.linear(x, w)
+    for i in range(0, n, 1 << 28):
+        assert torch.equal(y[0, i:i + (1 << 28)], (3.0 * w[i:i + (1 << 28), 5].float()).bfloat16())

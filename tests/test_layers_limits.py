@@ -53,3 +53,16 @@ def test_a_weights_gradient_from_one_row_of_any_length_is_taken(k):
     """From codes as from the row itself: no other row lies behind it."""
     wide = dict(m=1, n=1, k=k, d_stride=1, dw_stride=k)
     assert call("linear_weight_gradient", **wide) == call("linear_weight_gradient", x=P, x_stride=k, x_blob=None, **wide) == EHIP
+
+
+@no_gpu
+@pytest.mark.parametrize("n", [(1 << 30) - 15, 1 << 30])
+@pytest.mark.parametrize("m", [1, 17])
+def test_few_rows_by_as_many_as_there_may_be_are_taken(m, n):
+    given = dict(m=m, n=n, k=8, x_stride=8, w_stride=8, r_stride=n, y_stride=n, pre_blob=None)
+    assert call("linear", **given) == EHIP
+
+
+def test_more_tiles_than_are_counted_are_refused_ahead_of_every_launch():
+    """(Rows of fewer than eight values are copied first: with a GPU, that launch would not refuse.)"""
+    assert call("linear", m=1 << 30, n=1 << 30, k=5, x_stride=5, w_stride=5, r_stride=1 << 30, y_stride=1 << 30, pre_blob=None, kind=0) == ELIMIT
