@@ -26,7 +26,7 @@ from .mx4 import _buffer, _elsewhere, _flat, _on_gpu, _stream_of
 
 ACTIVATIONS = {"gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 _TYPES = {torch.bfloat16: MX4_BF16, torch.float16: MX4_F16, torch.float32: MX4_F32}
-_STRIDE_MOST = 1 << 23  # of the operands of products
+_STRIDE_MOST = 1 << 23  # elements between the rows of a product's operands: fewer
 _PLAIN = torch.contiguous_format
 
 
@@ -404,5 +404,7 @@ def linear(x, weight, bias=None, activation=None, residual=None, saved="codes"):
         with torch.cuda.device(at):
             return linear(x, weight, bias, activation, residual, saved)
     if _differentiable(x, weight, bias, residual):
+        if shape[0] >= _STRIDE_MOST and (x.requires_grad or weight.requires_grad) and x.shape[:-1].numel() > 1:
+            raise ValueError(f"gradients of rows and weight are products of the result's gradient, whose rows must be fewer than {_STRIDE_MOST} values long, not {shape[0]}")
         return _Linear.apply(x, weight, bias, residual, act, codes, kind, bkind)
     return _linear(x, _operand(x), _operand(weight), _adjacent(bias), None if residual is None else _flat(residual), act, kind, bkind, LINEAR_SERVED, None, None)

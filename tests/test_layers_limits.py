@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2508_00806_amd as adacc
+from paper_2508_00806_amd import layers
 from test_layers_host import BIG, CALLS, P
 
 EHIP, ELIMIT = adacc.EHIP, adacc.ELIMIT
@@ -66,3 +67,35 @@ def test_few_rows_by_as_many_as_there_may_be_are_taken(m, n):
 def test_more_tiles_than_are_counted_are_refused_ahead_of_every_launch():
     """(Rows of fewer than eight values are copied first: with a GPU, that launch would not refuse.)"""
     assert call("linear", m=1 << 30, n=1 << 30, k=5, x_stride=5, w_stride=5, r_stride=1 << 30, y_stride=1 << 30, pre_blob=None, kind=0) == ELIMIT
+
+
+# ---------------------------------------------------------------- the layers
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the library's functions that would have been called, with tensors in host memory."""
+    seen = []
+    monkeypatch.setattr(layers, "_on_gpu", lambda x: None)
+    monkeypatch.setattr(layers, "_stream_of", lambda x: 0)
+    monkeypatch.setattr(layers, "_call", lambda name, *args: seen.append(name))
+    return seen
+
+
+def t(*shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def test_a_forward_pass_whose_gradients_would_be_refused_is_refused(calls):
+    """The result's gradient is an operand of both products of the backward pass, and its rows lie apart as far as they are long."""
+    n = 1 << 23
+    for x, w in ((t(2, 8).requires_grad_(), t(1, 8).expand(n, 8)), (t(2, 8), t(1, 8).requires_grad_().expand(n, 8)), (t(2, 1, 8).requires_grad_(), t(1, 8).expand(n, 8))):
+        with pytest.raises(ValueError, match="fewer than"):
+            layers.linear(x, w)
+    assert calls == []
+    x, w = t(2, 8).requires_grad_(), t(1, 8).expand(n, 8)
+    with torch.no_grad():
+        layers.linear(x, w)
+    layers.linear(x[:1], w)                                 # one row: nothing lies apart
+    layers.linear(x, w[1:])
+    y = layers.linear(x.detach(), w, t(n).requires_grad_())  # sums of columns have no such limit
+    y.backward(y)
+    assert calls == ["linear"] * 4 + ["linear_columns"]
