@@ -864,6 +864,15 @@ def _vectors(a, b, what, n, kind):
     return (kb if a is None else ka), pa, pb
 
 
+def _stats(t, rows):
+    """Device pointer of the statistics of `rows` rows, or of None."""
+    if t is None:
+        return None
+    if t.shape != (rows, 2) or not t.is_contiguous() or _mx4_type(t) != MX4_F32:
+        raise ValueError(f"stats must be contiguous float32 of shape {(rows, 2)}, not {t.dtype} of {tuple(t.shape)}")
+    return t.data_ptr()
+
+
 def rows8_layout_of(rows: int, cols: int) -> CRows8Layout:
     L = CRows8Layout()
     _check(lib().adacc_rows8_layout_of(rows, cols, ctypes.byref(L)), "adacc_rows8_layout_of")
@@ -886,7 +895,7 @@ def norm_forward(x, weight, bias, eps: float, y, blob=None, stats=None, stream=N
     """y = layer norm of the rows of x, times weight, plus bias (either may be None).  blob: 8-bit rows of x are written; stats: float32 [rows, 2], mean and 1 / sigma."""
     kind = _mx4_type(x)
     wkind, w, b = _vectors(weight, bias, ("weight", "bias"), x.shape[1], kind)
-    _check(_layer("norm_forward")(kind, x.data_ptr(), *x.shape, _mx4_rows(x, "x"), wkind, w, b, float(eps), *_matrix(y, "y", x), *_mx4_blob(blob), _ptr(stats), _stream(stream)),
+    _check(_layer("norm_forward")(kind, x.data_ptr(), *x.shape, _mx4_rows(x, "x"), wkind, w, b, float(eps), *_matrix(y, "y", x), *_mx4_blob(blob), _stats(stats, x.shape[0]), _stream(stream)),
            "adacc_norm_forward")
 
 
@@ -901,7 +910,7 @@ def norm_backward(x, blob, weight, stats, dy, dx=None, dweight=None, dbias=None,
     rows, cols = dy.shape
     wkind, w, dw = _vectors(weight, dweight, ("weight", "dweight"), cols, kind)
     wkind, db = (wkind, None) if dbias is None else _vectors(weight if weight is not None else dweight, dbias, ("weight", "dbias"), cols, kind)[::2]
-    _check(_layer("norm_backward")(kind, *_matrix(x, "x", dy), *_mx4_blob(blob), rows, cols, wkind, w, _ptr(stats), dy.data_ptr(), _mx4_rows(dy, "dy"), *_matrix(dx, "dx", dy),
+    _check(_layer("norm_backward")(kind, *_matrix(x, "x", dy), *_mx4_blob(blob), rows, cols, wkind, w, _stats(stats, rows), dy.data_ptr(), _mx4_rows(dy, "dy"), *_matrix(dx, "dx", dy),
                                    dw, db, *_mx4_blob(workspace), _stream(stream)), "adacc_norm_backward")
 
 

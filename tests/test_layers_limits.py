@@ -99,3 +99,27 @@ def test_a_forward_pass_whose_gradients_would_be_refused_is_refused(calls):
     y = layers.linear(x.detach(), w, t(n).requires_grad_())  # sums of columns have no such limit
     y.backward(y)
     assert calls == ["linear"] * 4 + ["linear_columns"]
+
+
+# ---------------------------------------------------------------- the binding
+@pytest.mark.parametrize("stats", [t(6, 2, dtype=torch.float32), t(7, dtype=torch.float32), t(14, dtype=torch.float32), t(7, 2), t(2, 7, dtype=torch.float32).t(), t(7, 3, dtype=torch.float32)[:, :2],
+                                   t(7, 2, dtype=torch.float64)], ids=range(7))
+def test_statistics_that_are_not_two_numbers_a_row_are_refused(monkeypatch, stats):
+    def reached(*args):
+        raise AssertionError("the library was reached")
+    monkeypatch.setattr(adacc, "_layer", lambda name: reached)
+    monkeypatch.setattr(adacc, "_stream", lambda s: 0)
+    for call in (lambda: adacc.norm_forward(t(7, 8), None, None, 1e-5, t(7, 8), stats=stats), lambda: adacc.norm_backward(t(7, 8), None, None, stats, t(7, 8), dx=t(7, 8))):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+
+
+def test_statistics_reach_the_library(monkeypatch):
+    seen = []
+    monkeypatch.setattr(adacc, "_layer", lambda name: lambda *args: seen.append(args) or 0)
+    monkeypatch.setattr(adacc, "_stream", lambda s: 0)
+    stats = t(7, 2, dtype=torch.float32)
+    adacc.norm_forward(t(7, 8), None, None, 1e-5, t(7, 8), stats=stats)
+    adacc.norm_forward(t(7, 8), None, None, 1e-5, t(7, 8))
+    adacc.norm_backward(t(7, 8), None, None, stats, t(7, 8), dx=t(7, 8))
+    assert seen[0][13] == stats.data_ptr() and seen[1][13] is None and seen[2][9] == stats.data_ptr()
