@@ -132,6 +132,7 @@ class Rows8:
 
     def restore(self, dtype=torch.bfloat16):
         """The values that the codes stand for."""
+        _on_gpu(self.blob)
         if _elsewhere(self.blob):
             with torch.cuda.device(self.blob.get_device()):
                 return self.restore(dtype)

@@ -101,6 +101,16 @@ def test_a_forward_pass_whose_gradients_would_be_refused_is_refused(calls):
     assert calls == ["linear"] * 4 + ["linear_columns"]
 
 
+def test_codes_that_were_moved_to_host_memory_are_not_restored_there(monkeypatch):
+    seen = []
+    monkeypatch.setattr(layers, "_stream_of", lambda x: 0)
+    monkeypatch.setattr(layers, "_call", lambda name, *args: seen.append(name))
+    kept = layers.Rows8(t(2048, dtype=torch.uint8), (6, 64))
+    with pytest.raises(ValueError, match="GPU"):
+        kept.restore()
+    assert seen == []
+
+
 # ---------------------------------------------------------------- the binding
 @pytest.mark.parametrize("stats", [t(6, 2, dtype=torch.float32), t(7, dtype=torch.float32), t(14, dtype=torch.float32), t(7, 2), t(2, 7, dtype=torch.float32).t(), t(7, 3, dtype=torch.float32)[:, :2],
                                    t(7, 2, dtype=torch.float64)], ids=range(7))
