@@ -18,6 +18,7 @@ Plumbing only: buffers and calls; every step runs in the HIP kernels.
 import functools
 
 import torch
+from torch import _C
 from torch.autograd import forward_ad
 
 from . import ACT_GELU, ACT_GELU_TANH, ACT_NONE, ACT_SILU, LINEAR_ROWS_GRADIENT, LINEAR_SERVED, LINEAR_TRAINED, LINEAR_WEIGHT_GRADIENT, MX4_BF16, MX4_F16, MX4_F32
@@ -96,6 +97,8 @@ def _differentiable(*tensors):
 
 
 def _check_type(x, most=MX4_F32):
+    if _C._get_tracing_state() is not None:
+        raise RuntimeError("a layer's call can not be recorded by torch.jit.trace, which sees the result's allocation alone; it can be captured into a graph")
     _on_gpu(x)
     kind = _TYPES.get(x.dtype, MX4_F32 + 1)
     if kind > most:

@@ -111,6 +111,17 @@ def test_codes_that_were_moved_to_host_memory_are_not_restored_there(monkeypatch
     assert seen == []
 
 
+@pytest.mark.filterwarnings("ignore")
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("call", [lambda x: layers.layer_norm(x), lambda x: layers.activation(x), lambda x: layers.gated(x), lambda x: layers.linear(x, x),
+                                  lambda x: (x, layers.compress(x))[0]], ids=["layer_norm", "activation", "gated", "linear", "compress"])
+def test_a_trace_that_is_recorded_is_refused_in_words(calls, call, grad):
+    """The library's call is none of torch's operators: what was recorded would give back memory that nothing has written."""
+    with pytest.raises(RuntimeError, match="torch.jit.trace"):
+        torch.jit.trace(call, (t(6, 64).requires_grad_(grad),))
+    assert calls == []
+
+
 # ---------------------------------------------------------------- the binding
 @pytest.mark.parametrize("stats", [t(6, 2, dtype=torch.float32), t(7, dtype=torch.float32), t(14, dtype=torch.float32), t(7, 2), t(2, 7, dtype=torch.float32).t(), t(7, 3, dtype=torch.float32)[:, :2],
                                    t(7, 2, dtype=torch.float64)], ids=range(7))
