@@ -177,10 +177,11 @@ class _LayerNorm(torch.autograd.Function):
         w = _adjacent(weight)
         cols = x.shape[-1]
         n = x.shape[:-1].numel()
-        blob = _blob(n, cols, x.device) if codes else None
+        need = ctx.needs_input_grad[0] or ctx.needs_input_grad[1]  # (the bias's gradient takes nothing of x)
+        blob = _blob(n, cols, x.device) if codes and need else None
         stats = torch.empty((n, 2), dtype=torch.float32, device=x.device)
         y = _normed(x, kind, wkind, w, _adjacent(bias), eps, blob, stats)
-        ctx.save_for_backward(None if codes else x, blob, stats, w)
+        ctx.save_for_backward(x if need and not codes else None, blob, stats, w)
         ctx.kinds = kind, wkind
         return y
 
@@ -192,7 +193,10 @@ class _LayerNorm(torch.autograd.Function):
         kind, wkind = ctx.kinds
         rows = _flat(dy)
         n, cols = rows.shape
-        x = None if x is None else _flat(x)
+        if x is not None:
+            x = _flat(x)
+        elif blob is None:
+            x = rows  # (something of x's shape: db alone is wanted)
         dx = torch.empty_like(dy, memory_format=_PLAIN) if need_x else None
         wtype = torch.float32 if wkind == MX4_F32 else dy.dtype
         dw = torch.empty(cols, dtype=wtype, device=dy.device) if need_w else None
@@ -254,6 +258,8 @@ class _Activation(torch.autograd.Function):
         a8 = _blob(*a.shape, x.device) if codes else None
         u8 = _blob(*a.shape, x.device) if codes and gated else None
         y = _activated(x, a, u, act, kind, a8, u8)
+        if gated == 1 and not ctx.needs_input_grad[0]:  # up's gradient takes nothing of up
+            up = u8 = None
         ctx.save_for_backward(*((None, None) if codes else (x, up)), a8, u8)
         ctx.how = act, kind, gated, x.shape
         return y
@@ -272,6 +278,8 @@ class _Activation(torch.autograd.Function):
             dx = torch.empty(shape, dtype=dy.dtype, device=dy.device)
             da, du = _halves(_flat(dx))
         else:
+            if gated and up is None and u8 is None:
+                u, u8 = (None, a8) if x is None else (rows, None)  # (something of up's shape)
             if need_x:
                 dx = torch.empty_like(dy, memory_format=_PLAIN)
                 da = _flat(dx)

@@ -204,3 +204,39 @@ def test_one_row_by_as_many_as_there_may_be():
     y = layers.linear(x, w)
     for i in range(0, n, 1 << 28):
         assert torch.equal(y[0, i:i + (1 << 28)], (3.0 * w[i:i + (1 << 28), 5].float()).bfloat16())
+
+
+# ---------------------------------------------------------------- what no wanted gradient takes is not kept
+def kept_by(call):
+    """(result, bytes of every tensor that is kept for the backward pass)"""
+    kept = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t.nbytes) or t, lambda t: t):
+        y = call()
+    return y, sorted(kept)
+
+
+@pytest.mark.parametrize("saved", ["codes", "input"])
+@pytest.mark.parametrize("cols", [96, 700, 3001, 17000])
+def test_a_norm_whose_bias_alone_is_trained_keeps_nothing_of_its_rows(cols, saved):
+    x, w, b, dy = rand((33, cols), torch.bfloat16, 1), rand((cols,), torch.bfloat16, 2) + 1, rand((cols,), torch.bfloat16, 3), rand((33, cols), torch.bfloat16, 4)
+    every = [t.clone().requires_grad_() for t in (x, w, b)]
+    y = layers.layer_norm(*every, saved=saved)
+    want = torch.autograd.grad(y, every, dy)[2]
+    got, kept = kept_by(lambda: layers.layer_norm(x, w, b.requires_grad_(), saved=saved))
+    assert kept == sorted([33 * 8, w.nbytes]) and torch.equal(got, y)
+    assert torch.equal(torch.autograd.grad(got, b, dy)[0], want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("saved", ["codes", "input"])
+def test_a_gated_activation_of_which_up_alone_is_trained_keeps_the_gate_alone(saved, dtype):
+    t = TYPES[dtype]
+    x, u, dy = rand((5, 9, 301), t, 1), rand((5, 9, 301), t, 2), rand((5, 9, 301), t, 3)
+    both = [v.clone().requires_grad_() for v in (x, u)]
+    y = layers.gated(*both, "gelu", saved=saved)
+    want = torch.autograd.grad(y, both, dy)
+    got, kept = kept_by(lambda: layers.gated(x, u.requires_grad_(), "gelu", saved=saved))
+    assert kept == [layers.compress(x).nbytes if saved == "codes" else x.nbytes] and torch.equal(got, y)
+    assert torch.equal(torch.autograd.grad(got, u, dy)[0], want[1])
+    got, kept = kept_by(lambda: layers.gated(x.requires_grad_(), u.detach(), "gelu", saved=saved))  # the gate's takes both
+    assert len(kept) == 2 and torch.equal(torch.autograd.grad(got, x, dy)[0], want[0])
