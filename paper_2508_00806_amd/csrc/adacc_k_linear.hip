@@ -617,8 +617,8 @@ __global__ __launch_bounds__(kThreads) void lin_join_kernel(JoinArgs p) {
 JoinFn join_fn(uint32_t type) { return type == kTypeF16 ? lin_join_kernel<kTypeF16> : lin_join_kernel<kTypeBf16>; }
 
 // ------------------------------------------------------------------ few rows
-// A workgroup takes 16 * NS rows of w and up to 16 * MS rows of x; its wavefronts share the contraction, U steps of 32 at a time in turn, and add their sums up in LDS, in the
-// wavefronts' order.  Values go from memory to the operand registers: lane (r, q) = (lane % 16, lane / 16) reads values 8 q to 8 q + 7 of the step of its row.  A turn's loads
+// Where nothing is kept of what an activation is given.  A workgroup takes 16 * NS rows of w and up to 16 * MS rows of x; its wavefronts share the contraction, U steps of 32 at a time in turn,
+// and add their sums up in LDS, in the wavefronts' order.  Values go from memory to the operand registers: lane (r, q) = (lane % 16, lane / 16) reads values 8 q to 8 q + 7 of the step of its row.  A turn's loads
 // are under way while the turn before is multiplied.
 //   What bounds it is reading w once, from many compute units at a time: one row by 11008 x 4096 18 us (5.0 TB/s), by 4096 x 4096 8.5; 16 rows by 4096 x 11008 22 to 26 (4.1 to 3.4), of which 6 are x,
 // which every workgroup reads.  Tried for these two: 12 and 16 wavefronts (19.8 and 21.2; 26.2 and 26.3); 32 and 64 columns a workgroup (25.0 and 24.5; 33.9 and 52.4); each workgroup
@@ -740,12 +740,9 @@ __global__ __launch_bounds__(8 * kWave) void lin_few_kernel(ProductArgs p) {
     for (uint32_t u = 0; u < waves; ++u) v += sums[(u * kRows + row) * kCols + in];
     const uint32_t col = col0 + in;
     if (p.e.bias) v += load1(p.e.btype, p.e.bias, col);
-    if (p.e.act != kActNone) {
-      if (p.e.pre.at) store1<TYPE>(p.e.pre.at, (uint64_t)(row0 + row) * p.e.pre.stride + col, v);
-      if (p.e.act == kActGelu) activate<kActGelu, false, false>(v, &v, &none);
-      else if (p.e.act == kActGeluTanh) activate<kActGeluTanh, false, false>(v, &v, &none);
-      else activate<kActSilu, false, false>(v, &v, &none);
-    }
+    if (p.e.act == kActGelu) activate<kActGelu, false, false>(v, &v, &none);
+    else if (p.e.act == kActGeluTanh) activate<kActGeluTanh, false, false>(v, &v, &none);
+    else if (p.e.act == kActSilu) activate<kActSilu, false, false>(v, &v, &none);
     if (p.e.residual.at) v += load1<TYPE>(p.e.residual.at, (uint64_t)(row0 + row) * p.e.residual.stride + col);
     store1<TYPE>(p.e.out.at, (uint64_t)(row0 + row) * p.e.out.stride + col, v);
   }
