@@ -2,8 +2,9 @@
 // One pass over the data either way; binary32 in registers, rounded once.
 //
 // What bounds them is memory.  Sixteen lanes hold a group of 128, eight values a lane, so that its largest magnitude takes four exchanges in the vector unit; a lane has a place in four groups, whose loads
-// are all under way before the first is used; data pass with the streaming hint.  bfloat16, with codes: GELU of [8192, 16384] 107 us forward and 108 backward (6.3 TB/s both); SiLU gated [16384, 11008] 226
-// and 238 (6.4 and 6.1); a copy runs at 6.3.  Rows whose length is no multiple of eight: [1999, 4093] 12.0 and 11.6 us.
+// are all under way before the first is used; data pass with the streaming hint.  bfloat16, with codes: GELU of [8192, 16384] 110 us forward and 111 backward (6.1 TB/s both; two products fewer in its
+// tail, 107 and 108), SiLU 101 and 97; SiLU gated [16384, 11008] 226 and 238 (6.4 and 6.1); a copy runs at 6.3.  binary32, [8192, 8192]: GELU 118 and 109 (5.2, 5.6), SiLU gated 176 and 166 (5.4, 5.7).
+// Rows whose length is no multiple of eight: [1999, 4093] 12.0 and 11.6 us; [8191, 8191] 69 and 66 (4.9, 5.1).
 #include "adacc_layers.hpp"
 
 namespace adacc {

@@ -266,10 +266,11 @@ __device__ __forceinline__ void lin_band(uint32_t id, uint32_t m_tiles, uint32_t
 // ------------------------------------------------------------------ tiles
 // Four wavefronts, two by two, each S x S tiles of 32 x 32 (S = 4, or 2).  Row S * r + i of a wavefront's rows is row r of its tile i, so that a lane's S columns of
 // the results lie side by side.
-//   What bounds the tile of 256 (32 x 32 x 16 products, a step of 64 in 2048 cycles of the matrix unit, one workgroup a compute unit, 496 registers a lane): power first.  8192^3 0.86 ms (1.28 PFLOP/s;
-// the library's product 0.76, the same kernel on zeros 1.6 PFLOP/s).  Then the one wavefront of a SIMD: whatever it issues beside its products it issues between them, and a load or
-// store that has to wait stops them.  bfloat16, us: 16384 x 11008 x 4096 1215 (library 1126 to 1166), with SiLU 1223, with GELU and its codes 1350; 8192 x 8192 x 2048 242 (189 to 194), with GELU 283, with
-// GELU and codes 317: there the results and a tile's first loads are a seventh of the time, and nothing else runs under them.  Gradients: dx 221 (library 203 to 256), dw 225 (247 to 291), from codes 252.
+//   What bounds the tile of 256 (32 x 32 x 16 products, a step of 64 in 2048 cycles of the matrix unit, one workgroup a compute unit, 496 registers a lane): the one wavefront of a SIMD, and
+// power.  8192^3 of N(0, 1) 0.82 ms, 1.33 PFLOP/s (the library's product 0.67, 1.65), of zeros, where power is no limit, 0.60, 1.83 PFLOP/s (0.49, 2.27): random data cost both a quarter, and on both this
+// kernel is a fifth behind.  Whatever the wavefront issues beside its products it issues between them, and a load or store that has to wait stops them.  bfloat16, us: 16384 x 11008 x 4096 1168
+// to 1215 (library 1085 to 1166), with SiLU 1223, with GELU and its codes 1350; 8192 x 8192 x 2048 245 (189 to 194), with GELU 281, with GELU and codes, or its input kept, 319: there the results and a
+// tile's first loads are a seventh of the time, and nothing else runs under them.  Gradients: dx 220 (library 203 to 256), dw 220 (247 to 291), from codes 245.
 //   Tried: loads that pass the registers by (no faster: the same addresses are taken at the same rate), two register sets for the step's loads (the sums no longer fit), results through LDS for
 // this tile as for that of 128 (260 instead of 239).
 template <uint32_t TILE>
@@ -621,7 +622,7 @@ JoinFn join_fn(uint32_t type) { return type == kTypeF16 ? lin_join_kernel<kTypeF
 // and add their sums up in LDS, in the wavefronts' order.  Values go from memory to the operand registers: lane (r, q) = (lane % 16, lane / 16) reads values 8 q to 8 q + 7 of the step of its row.  A turn's loads
 // are under way while the turn before is multiplied.
 //   What bounds it is reading w once, from many compute units at a time: one row by 11008 x 4096 18 us (5.0 TB/s), by 4096 x 4096 8.5; 16 rows by 4096 x 11008 22 to 26 (4.1 to 3.4), of which 6 are x,
-// which every workgroup reads.  Tried for these two: 12 and 16 wavefronts (19.8 and 21.2; 26.2 and 26.3); 32 and 64 columns a workgroup (25.0 and 24.5; 33.9 and 52.4); each workgroup
+// which every workgroup reads; 17 rows by 11008 x 4096 23, 32 rows 26 (3.9 and 3.5), by 4096 x 4096 11 and 14, 32 by 4096 x 11008 32: x again, twice as much of it.  Tried for the first two: 12 and 16 wavefronts (19.8 and 21.2; 26.2 and 26.3); 32 and 64 columns a workgroup (25.0 and 24.5; 33.9 and 52.4); each workgroup
 // beginning elsewhere in the contraction (20.4; 24.9).
 template <uint32_t MS, uint32_t NS>
 struct FewTurn {

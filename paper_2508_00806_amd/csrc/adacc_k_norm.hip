@@ -11,7 +11,10 @@
 //
 // What bounds both is memory.  Forward and backward pass in turn, with the parameters' gradients: bfloat16 [32768, 2048] 124 us from the input as it was (5.4 TB/s), 137 from codes (4.9), [8192, 8192] 120 (5.6),
 // binary16 [8191, 11008] 170 (5.3); a copy runs at 6.3.  Results go to memory with the streaming hint: without it a forward pass that follows a backward pass takes 90 us for [8191, 11008] instead of 64.
-// Rows of 1999 x 4093 binary32: 17 and 27.  Two rows ahead, or half and twice as many workgroups, were slower.
+// Rows of 1999 x 4093 binary32: 17 and 28.  Two rows ahead, or half and twice as many workgroups, were slower.
+//   Fewer rows are further from that: bfloat16 [8191, 2048] forward with codes 17 us (4.8 TB/s), backward 36 (2.4), of which joining the parameters' sums is 7; rows that eight does not divide add to the forward
+// pass, [8191, 2047] 21 and 37.  More than 16384 columns, read in pieces three times: [4096, 20480] served 105 us (3.2 TB/s of one reading), forward with codes 123, backward from codes 183, from the input 209;
+// [4096, 20479] 139, 157, 232, 304; [4096, 16384], in registers, 42, 56, 80, 94.
 #include "adacc_layers.hpp"
 
 namespace adacc {

@@ -187,7 +187,8 @@ static double lin_time_128(uint64_t m, uint64_t n, uint64_t steps, uint64_t spli
 static LinPlan lin_plan(uint64_t m, uint64_t n, uint64_t k, bool may_be_few) {
   LinPlan p;
   std::memset(&p, 0, sizeof p);
-  p.few = may_be_few && k >= kLinShort && m <= 32;  // (64 x 4096 x 4096: 22 us, in tiles 16; 32 by 11008 x 4096 29 and 32)
+  // up to 32 rows: 64 x 4096 x 4096 22 us, in tiles 16; 32 by 4096 x 4096 14, 33 in tiles 15; 32 by 11008 x 4096 26, 33 in tiles 24.  (By 4096 x 11008, 32 rows take 32, 64 in tiles 26.)
+  p.few = may_be_few && k >= kLinShort && m <= 32;
   p.splits = 1;
   if (p.few) {
     p.ms = m <= 16 ? 1u : 2u;

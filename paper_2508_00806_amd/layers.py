@@ -394,7 +394,8 @@ def linear(x, weight, bias=None, activation=None, residual=None, saved="codes"):
     """act(x [..., k] weight [n, k]^T + bias [n]) + residual [..., n], in one pass; sums in binary32, rounded once.
 
     x, weight and residual: bfloat16 or float16, all of one type; bias: of that type or float32.  activation: None, "gelu", "gelu_tanh" or "silu".  Gradients reach x, weight, bias
-    and residual.  saved="codes": x (for the weight's gradient) and what the activation is given are kept in 8 bits."""
+    and residual.  saved="codes": x (for the weight's gradient) and what the activation is given are kept in 8 bits; "input": in x's type, finite values beyond its range as its largest.
+    The gradient of what the activation is given is rounded to x's type, as the products take it that make those of x and weight; the bias's is its sum before that."""
     act, codes = ACT_NONE if activation is None else _kind(activation), _codes(saved)
     kind = bkind = _check_type(x, MX4_F16)
     shape = weight.shape

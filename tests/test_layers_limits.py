@@ -1,4 +1,5 @@
-"""Calls at the limits of the layers' sizes; no GPU is needed, and none may be there: what is taken would be launched on addresses that do not exist, and fails where there is no GPU."""
+"""Calls at the limits of the layers' sizes, and what the layers and their binding refuse; no GPU is needed.  What is taken would be launched, on addresses that do not exist: without a GPU the launch
+fails, with one those tests are skipped."""
 import pytest
 import torch
 
