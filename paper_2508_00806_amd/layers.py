@@ -96,10 +96,14 @@ def _differentiable(*tensors):
     return False
 
 
-def _check_type(x, most=MX4_F32):
+def _check_place(x):
     if _C._get_tracing_state() is not None:
         raise RuntimeError("a layer's call can not be recorded by torch.jit.trace, which sees the result's allocation alone; it can be captured into a graph")
     _on_gpu(x)
+
+
+def _check_type(x, most=MX4_F32):
+    _check_place(x)
     kind = _TYPES.get(x.dtype, MX4_F32 + 1)
     if kind > most:
         raise TypeError(f"{', '.join(str(t)[6:] for t, k in _TYPES.items() if k <= most)} is needed, not {x.dtype}")
@@ -135,7 +139,7 @@ class Rows8:
 
     def restore(self, dtype=torch.bfloat16):
         """The values that the codes stand for."""
-        _on_gpu(self.blob)
+        _check_place(self.blob)
         if _elsewhere(self.blob):
             with torch.cuda.device(self.blob.get_device()):
                 return self.restore(dtype)

@@ -115,7 +115,8 @@ def test_codes_that_were_moved_to_host_memory_are_not_restored_there(monkeypatch
 @pytest.mark.filterwarnings("ignore")
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("call", [lambda x: layers.layer_norm(x), lambda x: layers.activation(x), lambda x: layers.gated(x), lambda x: layers.linear(x, x),
-                                  lambda x: (x, layers.compress(x))[0]], ids=["layer_norm", "activation", "gated", "linear", "compress"])
+                                  lambda x: (x, layers.compress(x))[0], lambda x: layers.Rows8(t(8, dtype=torch.uint8), (6, 64)).restore() + x],
+                         ids=["layer_norm", "activation", "gated", "linear", "compress", "restore"])
 def test_a_trace_that_is_recorded_is_refused_in_words(calls, call, grad):
     """The library's call is none of torch's operators: what was recorded would give back memory that nothing has written."""
     with pytest.raises(RuntimeError, match="torch.jit.trace"):
